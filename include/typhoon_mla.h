@@ -362,6 +362,93 @@ int typhoon_mla_expand_query_rows(const int32_t* block_table, const int32_t* seq
                                   int32_t* seq_lens_rows, void* stream);
 
 /*
+ * ---- Around a step: rotary positions, the paged cache, drafted tokens ----
+ *
+ * The paged cache as typhoon_mla_decode reads it (16-bit), or with the latent rows in 8 bits.
+ *
+ *   ckv_pages      latent rows, token (page p, slot s) at (p * page_size + s) * ckv_token_stride elements, 512 wide:
+ *                  bf16, or with ckv_exponents non-NULL OCP E4M3 codes (1-4-3 bits, bias 7, no infinities, largest value 448)
+ *   kpe_pages      bf16 rope keys, same addressing with kpe_token_stride, 64 wide
+ *   ckv_exponents  NULL, or one byte per token [num_pages, page_size] contiguous, 16-byte aligned: the row's codes stand for
+ *                  code * 2^(byte - 127); 255: the row is not finite (every value NaN)
+ *   strides        in elements (of 2 bytes or 1), multiples of 16 bytes, >= 512 / 64; base pointers 16-byte aligned
+ */
+typedef struct {
+    void* ckv_pages;
+    void* kpe_pages;
+    uint8_t* ckv_exponents;
+    int64_t ckv_token_stride, kpe_token_stride;
+    int32_t page_size;   /* 64 or 128 */
+    int32_t num_pages;
+} typhoon_mla_cache_t;
+
+/*
+ * Rotary positions.  Pair i (0 <= i < d_rot / 2) of a row's 64 rope dims is turned by position * f_i radians and multiplied by
+ * `scale`: (x, y) -> scale (x cos - y sin, x sin + y cos).  The pair is (2 i, 2 i + 1) with INTERLEAVED, (i, i + d_rot / 2) with
+ * HALF; dims d_rot .. 63 are copied.  Positions are any int32; angles are good to 4e-7 at every one of them.
+ * The structure is plain data (host); typhoon_mla_rope_init fills it.  A program with frequencies of its own writes
+ * turns[i] = f_i / (2 pi) * 2^64.
+ */
+enum { TYPHOON_MLA_ROPE_INTERLEAVED = 0, TYPHOON_MLA_ROPE_HALF = 1 };
+enum {
+    TYPHOON_MLA_ROPE_SCALE_NONE = 0,   /* f_i = base^(-2 i / d_rot) */
+    TYPHOON_MLA_ROPE_SCALE_LINEAR = 1, /* f_i / factor */
+    TYPHOON_MLA_ROPE_SCALE_NTK = 2,    /* base * factor^(d_rot / (d_rot - 2)) in place of base */
+    TYPHOON_MLA_ROPE_SCALE_YARN = 3    /* f_i below `low`, f_i / factor above `high`, a linear ramp over i between; low and high are
+                                          the pairs that turn beta_fast and beta_slow times over original_length positions,
+                                          d_rot ln(original_length / (2 pi beta)) / (2 ln base), rounded down and up and kept
+                                          within 0 .. d_rot - 1 */
+};
+typedef struct {
+    int32_t d_rot;       /* 16, 32, 48 or 64 */
+    int32_t layout;
+    float scale;
+    int32_t reserved;
+    uint64_t turns[32];
+} typhoon_mla_rope_t;
+
+/* Host, pure.  base > 1; factor >= 1 (LINEAR, NTK, YARN); original_length >= 1 and beta_fast >= beta_slow > 0 (YARN); scale finite
+ * (1; YaRN's attention factor where a model uses one).  INVALID_ARG otherwise, and *rope is left alone. */
+int typhoon_mla_rope_init(typhoon_mla_rope_t* rope /* host */, int32_t d_rot, int32_t layout, double base, int32_t scaling, double factor,
+                          double original_length, double beta_fast, double beta_slow, double scale);
+
+/*
+ * Query rows as a step takes them, from the rows of a projection: q_pe (64 wide) rotated into q_pe_out bf16 [T, H, 64], and, unless
+ * both are NULL, q_nope (128 wide) copied into q_nope_out bf16 [T, H, 128]; the outputs are contiguous.  Row (t, h) of an input
+ * starts at t * token_stride + h * head_stride elements (multiples of 8; with one projection of 192 per head both point into it).
+ * positions int32 [T].  Keys are rows with H = 1.  q_pe_out may be q_pe itself where that is contiguous; inputs and outputs do
+ * not overlap otherwise.  1 <= H <= 65536; T = 0 is allowed and does nothing.  Asynchronous on `stream`.
+ */
+int typhoon_mla_rope_queries(const typhoon_mla_rope_t* rope /* host */, const void* q_nope, int64_t nope_token_stride, int64_t nope_head_stride,
+                             const void* q_pe, int64_t pe_token_stride, int64_t pe_head_stride, const int32_t* positions, int64_t T,
+                             int32_t H, void* q_nope_out, void* q_pe_out, void* stream);
+
+/*
+ * Write T new tokens into the cache: latent row t (ckv, bf16, 512 wide, row stride ld_ckv) and rope key t (kpe, bf16, 64 wide, row
+ * stride ld_kpe; strides in elements, multiples of 8), rotated to positions[t] first unless rope and positions are both NULL,
+ * go to slot slots[t] = page * page_size + slot in page.  Negative slots are skipped (padding tokens); a slot at or past
+ * num_pages * page_size is not dereferenced and sets TYPHOON_MLA_STATUS_BAD_PAGE in *status (device word, may be NULL; it is
+ * only ORed into).  Slots of one call that are not negative differ from one another.
+ * With an 8-bit cache the row is encoded as it is written: the exponent is the smallest one for which the row's largest magnitude
+ * fits 448 (at least -126, byte 1), the codes are the row divided by that power of two, rounded to nearest even (and never to
+ * 2^128, which bf16 does not hold: 1.875 * 2^127 then); a row with an infinity or a NaN gets byte 255 and codes of zero.
+ * Asynchronous on `stream`; T = 0 is allowed and does nothing.
+ */
+int typhoon_mla_cache_append(const typhoon_mla_cache_t* cache /* host */, const void* ckv, int64_t ld_ckv, const void* kpe, int64_t ld_kpe,
+                             const typhoon_mla_rope_t* rope /* host */, const int32_t* positions, const int64_t* slots, int64_t T,
+                             int32_t* status, void* stream);
+
+/*
+ * Read T tokens back: row t of ckv_out (bf16, 512 wide, row stride ld_ckv) and of kpe_out (bf16, 64 wide, row stride ld_kpe) are
+ * the token in slot slots[t], zeros where that is negative or (with BAD_PAGE set in *status) at or past num_pages * page_size.  Slots
+ * may repeat.  An 8-bit row is widened exactly (values below 2^-126 to bf16's nearest).  For prompts that become a shared
+ * prefix (typhoon_mla_prepare_shared takes such rows), and, with typhoon_mla_cache_append without rotation, for moving accepted
+ * drafts to their places: encoding a row that was read back gives its values again.  Asynchronous on `stream`.
+ */
+int typhoon_mla_cache_read(const typhoon_mla_cache_t* cache /* host */, const int64_t* slots, int64_t T, void* ckv_out, int64_t ld_ckv,
+                           void* kpe_out, int64_t ld_kpe, int32_t* status, void* stream);
+
+/*
  * Device-side checks.  The handle owns one status word in device memory, zero after
  * typhoon_mla_prepare_shared.  Kernels never trap or assert; instead they OR a bit into the word:
  *   TYPHOON_MLA_STATUS_WAIT_EXPIRED  a bounded in-kernel wait ran out (every wait on a copy or a tensor-core

@@ -28,6 +28,17 @@ class Dims(C.Structure):
                 ("d_v", C.c_int32), ("kv_lora_rank", C.c_int32)]
 
 
+class Rope(C.Structure):
+    """typhoon_mla_rope_t"""
+    _fields_ = [("d_rot", C.c_int32), ("layout", C.c_int32), ("scale", C.c_float), ("reserved", C.c_int32), ("turns", C.c_uint64 * 32)]
+
+
+class Cache(C.Structure):
+    """typhoon_mla_cache_t"""
+    _fields_ = [("ckv_pages", C.c_void_p), ("kpe_pages", C.c_void_p), ("ckv_exponents", C.c_void_p), ("ckv_token_stride", C.c_int64),
+                ("kpe_token_stride", C.c_int64), ("page_size", C.c_int32), ("num_pages", C.c_int32)]
+
+
 class TyphoonMLAError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -56,6 +67,14 @@ def _load():
                                                   C.POINTER(vp)]
     lib.typhoon_mla_shared_storage_bytes.restype = sz
     lib.typhoon_mla_shared_storage_bytes.argtypes = [C.POINTER(Dims), i64, i32, C.POINTER(sz)]
+    lib.typhoon_mla_rope_init.restype = C.c_int
+    lib.typhoon_mla_rope_init.argtypes = [C.POINTER(Rope), i32, i32, f64, i32, f64, f64, f64, f64, f64]
+    lib.typhoon_mla_rope_queries.restype = C.c_int
+    lib.typhoon_mla_rope_queries.argtypes = [C.POINTER(Rope), vp, i64, i64, vp, i64, i64, vp, i64, i32, vp, vp, vp]
+    lib.typhoon_mla_cache_append.restype = C.c_int
+    lib.typhoon_mla_cache_append.argtypes = [C.POINTER(Cache), vp, i64, vp, i64, C.POINTER(Rope), vp, vp, i64, vp, vp]
+    lib.typhoon_mla_cache_read.restype = C.c_int
+    lib.typhoon_mla_cache_read.argtypes = [C.POINTER(Cache), vp, i64, vp, i64, vp, i64, vp, vp]
     lib.typhoon_mla_host_range_mapped.restype = C.c_int
     lib.typhoon_mla_host_range_mapped.argtypes = [vp, i64]
     lib.typhoon_mla_naive_plan_multi.restype = C.c_int
@@ -319,6 +338,134 @@ def typhoon_mla_decode_tree(levels, q_nope, q_pe, ckv_pages, kpe_pages, page_siz
         _ptr(out), _ptr(lse_out),
         _ptr(workspace), workspace.numel() * workspace.element_size(), _stream())
     _check(st, "typhoon_mla_decode_tree")
+
+
+# ---- around a step: rotary positions, the paged cache, drafted tokens
+ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+
+def _device() -> int:
+    return torch._C._cuda_getDevice()
+
+
+def _need(t: torch.Tensor, name: str, dtype, shape: tuple, dev: int, contiguous: bool = True) -> int:
+    """Address of a tensor of this type and shape on CUDA device `dev`; dense in its last dimension, contiguous altogether unless told
+    otherwise.  (These calls last a few microseconds on the device: a tensor that is as asked for costs half of one here.)"""
+    if t.dtype is dtype and t.get_device() == dev and t.shape == shape and (t.is_contiguous() or not contiguous and t.stride(-1) == 1):
+        return t.data_ptr()
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be a {dtype} tensor, got {t.dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on the current CUDA device ({dev}), got {t.device}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+    raise ValueError(f"{name} must be {'contiguous' if contiguous else 'dense in its last dimension'}")
+
+
+def _sizes(t: torch.Tensor, n: int, name: str) -> tuple:
+    if not isinstance(t, torch.Tensor) or t.dim() != n:
+        raise ValueError(f"{name} must be a tensor of {n} dimensions")
+    return t.shape
+
+
+def _steps(t: torch.Tensor) -> tuple:
+    """Strides of the first two of three dimensions (a dimension of extent 1 may have any)."""
+    return t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
+
+
+def typhoon_mla_rope_init(d_rot: int = 64, layout: str = "interleaved", base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                          original_length: float = 4096.0, beta_fast: float = 32.0, beta_slow: float = 1.0, scale: float = 1.0) -> Rope:
+    """Rotary settings: `d_rot` (16, 32, 48, 64) of the 64 rope dims, pairs "interleaved" or "half", `scaling` "none", "linear",
+    "ntk" or "yarn"."""
+    r = Rope()
+    _check(_lib.typhoon_mla_rope_init(C.byref(r), d_rot, ROPE_LAYOUTS[layout], base, ROPE_SCALINGS[scaling], factor, original_length,
+                                      beta_fast, beta_slow, scale), "typhoon_mla_rope_init")
+    return r
+
+
+def typhoon_mla_rope_queries(rope: Rope, q_pe: torch.Tensor, positions: torch.Tensor, q_pe_out: torch.Tensor,
+                             q_nope: Optional[torch.Tensor] = None, q_nope_out: Optional[torch.Tensor] = None) -> None:
+    """q_pe [T, H, 64] (any strides that are multiples of 8, such as a slice of a projection) rotated to positions int32 [T] into
+    q_pe_out; q_nope [T, H, 128] copied into q_nope_out.  q_pe_out may be q_pe."""
+    T, H, _ = _sizes(q_pe, 3, "q_pe")
+    dev, bf = _device(), torch.bfloat16
+    src = _need(q_pe, "q_pe", bf, (T, H, 64), dev, contiguous=False)
+    pos = _need(positions, "positions", torch.int32, (T,), dev)
+    dst = _need(q_pe_out, "q_pe_out", bf, (T, H, 64), dev)
+    nope, nope_out, steps = None, None, (0, 0)
+    if q_nope is not None or q_nope_out is not None:
+        if q_nope is None or q_nope_out is None:
+            raise ValueError("q_nope and q_nope_out go together")
+        nope = _need(q_nope, "q_nope", bf, (T, H, 128), dev, contiguous=False)
+        nope_out = _need(q_nope_out, "q_nope_out", bf, (T, H, 128), dev)
+        steps = _steps(q_nope)
+    st = _lib.typhoon_mla_rope_queries(rope, nope, *steps, src, *_steps(q_pe), pos, T, H, nope_out, dst,
+                                       torch._C._cuda_getCurrentRawStream(dev))
+    _check(st, "typhoon_mla_rope_queries")
+
+
+class PagedCache:
+    """The paged cache: ckv_pages [pages, page_size, 512] bf16, or uint8 E4M3 codes together with exponents uint8
+    [pages, page_size]; kpe_pages [pages, page_size, 64] bf16.  Both may be slices of wider rows (strides multiples of 16 bytes)."""
+
+    def __init__(self, ckv_pages: torch.Tensor, kpe_pages: torch.Tensor, exponents: Optional[torch.Tensor] = None):
+        pages, page, _ = _sizes(ckv_pages, 3, "ckv_pages")
+        dev = _device()
+        _need(ckv_pages, "ckv_pages", torch.bfloat16 if exponents is None else torch.uint8, (pages, page, 512), dev, contiguous=False)
+        _need(kpe_pages, "kpe_pages", torch.bfloat16, (pages, page, 64), dev, contiguous=False)
+        for t, name in ((ckv_pages, "ckv_pages"), (kpe_pages, "kpe_pages")):
+            if pages > 1 and t.stride(0) != page * t.stride(1):
+                raise ValueError(f"{name}: tokens must follow one another at one stride")
+        if exponents is not None:
+            _need(exponents, "exponents", torch.uint8, (pages, page), dev)
+        self.ckv_pages, self.kpe_pages, self.exponents, self.device = ckv_pages, kpe_pages, exponents, dev
+        self.struct = Cache(ckv_pages.data_ptr(), kpe_pages.data_ptr(), None if exponents is None else exponents.data_ptr(),
+                            ckv_pages.stride(1), kpe_pages.stride(1), page, pages)
+
+    @property
+    def page_size(self) -> int:
+        return self.struct.page_size
+
+    def on(self, dev: int) -> Cache:
+        """The C structure, for a call on this device."""
+        if self.device != dev:
+            raise ValueError(f"the cache must be on the current CUDA device ({dev}), it is on {self.device}")
+        return self.struct
+
+
+def typhoon_mla_cache_append(cache: PagedCache, ckv: torch.Tensor, kpe: torch.Tensor, slots: torch.Tensor, rope: Optional[Rope] = None,
+                             positions: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
+    """Latent rows ckv [T, 512] and rope keys kpe [T, 64] (rotated to positions int32 [T] if `rope` is given) go to slots int64 [T]
+    (page * page_size + slot in page; negative: skipped; otherwise all different).  status: int32 [1], ORed into."""
+    T, _ = _sizes(ckv, 2, "ckv")
+    dev, bf = _device(), torch.bfloat16
+    if (rope is None) != (positions is None):
+        raise ValueError("rope and positions go together")
+    st = _lib.typhoon_mla_cache_append(
+        cache.on(dev), _need(ckv, "ckv", bf, (T, 512), dev, contiguous=False), ckv.stride(0) if T > 1 else 512,
+        _need(kpe, "kpe", bf, (T, 64), dev, contiguous=False), kpe.stride(0) if T > 1 else 64, rope,
+        None if positions is None else _need(positions, "positions", torch.int32, (T,), dev), _need(slots, "slots", torch.int64, (T,), dev), T,
+        None if status is None else _need(status, "status", torch.int32, (1,), dev), torch._C._cuda_getCurrentRawStream(dev))
+    _check(st, "typhoon_mla_cache_append")
+
+
+def typhoon_mla_cache_read(cache: PagedCache, slots: torch.Tensor, ckv_out: Optional[torch.Tensor] = None,
+                           kpe_out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """(ckv bf16 [T, 512], kpe bf16 [T, 64]): the tokens in slots int64 [T] (negative: zeros)."""
+    T, = _sizes(slots, 1, "slots")
+    dev, bf = _device(), torch.bfloat16
+    at = _need(slots, "slots", torch.int64, (T,), dev)
+    if ckv_out is None:
+        ckv_out = torch.empty(T, 512, dtype=bf, device=slots.device)
+    if kpe_out is None:
+        kpe_out = torch.empty(T, 64, dtype=bf, device=slots.device)
+    st = _lib.typhoon_mla_cache_read(
+        cache.on(dev), at, T, _need(ckv_out, "ckv_out", bf, (T, 512), dev, contiguous=False), ckv_out.stride(0) if T > 1 else 512,
+        _need(kpe_out, "kpe_out", bf, (T, 64), dev, contiguous=False), kpe_out.stride(0) if T > 1 else 64,
+        None if status is None else _need(status, "status", torch.int32, (1,), dev), torch._C._cuda_getCurrentRawStream(dev))
+    _check(st, "typhoon_mla_cache_read")
+    return ckv_out, kpe_out
 
 
 def typhoon_mla_host_staging_bytes(shared: SharedPrefix, B: int, max_pages: int) -> int:

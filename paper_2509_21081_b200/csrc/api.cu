@@ -80,6 +80,7 @@ int cuda_fail(cudaError_t e) {
 }  // namespace
 int tmla::api_cuda_fail(cudaError_t e) { return cuda_fail(e); }
 void tmla::api_set_last_launches(int n) { g_last_launches = n; }
+void tmla::api_adopt_settings() { tl_pdl = g_pdl.load(); }
 namespace {
 
 // ---- side stream and events of a handle -------------------------------------

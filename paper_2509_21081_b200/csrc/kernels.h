@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "../../include/typhoon_mla.h"
+
 namespace tmla {
 
 // Launch with the programmatic-stream-serialization attribute when enabled (see sm100::pdl_wait).  The switch is per
@@ -248,6 +250,10 @@ int noalloc_resolve_scratch_for_current_device();
 // TYPHOON_MLA_ERR_CUDA (returns that status) and the number of kernels the call launched, both per thread.
 int api_cuda_fail(cudaError_t e);
 void api_set_last_launches(int n);
+// Takes this thread's snapshot of the process-wide programmatic-launch switch (tl_pdl), before the first launch of a call.
+void api_adopt_settings();
+// Whether the fields of a paged cache are what its declaration asks for.
+bool cache_valid(const typhoon_mla_cache_t* cache);
 
 // Copies n <= 4 arrays (multiples of 4 bytes, 4-byte aligned) in one launch; either side may be device-visible host memory.
 // At the device's highest priority.
