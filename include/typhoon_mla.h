@@ -449,6 +449,35 @@ int typhoon_mla_cache_read(const typhoon_mla_cache_t* cache /* host */, const in
                            void* kpe_out, int64_t ld_kpe, int32_t* status, void* stream);
 
 /*
+ * One decode step for B requests with S drafted tokens each (1 <= S <= 64; S = 1: single tokens), over a 16-bit or an 8-bit cache.
+ * The cache holds the drafts as the last tokens of every suffix, seq_lens[b] counts them.  Query row (b, j), j < S, attends to
+ *   - the whole shared prefix,
+ *   - the committed tokens: suffix positions p < L - n,
+ *   - draft i (position L - n + i, 0 <= i < n) where bit i of its mask is set,
+ * with L = seq_lens[b] clamped to 0 .. max_pages * page_size, n = draft_lens[b] clamped to 0 .. S (S where draft_lens is NULL;
+ * drafts at negative positions do not exist).  tree_mask uint64 [B, S] (8-byte aligned); NULL: bits 0 .. j for row j (a chain).
+ * A tree of drafts has every row's bit for itself and for its ancestors; any other mask is allowed, one without bits included.
+ * A row that sees nothing at all gets a zero output and lse = -inf.  What a row does not see does not reach it, whatever
+ * it holds (NaN included); a row that sees a NaN becomes NaN (output and lse).  Rows j >= n are computed like the others.
+ *   q_nope bf16 [B * S, H, 128], q_pe bf16 [B * S, H, 64], out bf16 [B * S, H, 128], lse_out optional fp32 [B * S, H]: row b * S + j
+ *   block_table int32 [B, max_pages], seq_lens int32 [B]: per request (max_pages >= 1); bad page ids as in typhoon_mla_decode
+ *   mode  AUTO, ABSORB or HYBRID (NAIVE: INVALID_ARG)
+ *   workspace  typhoon_mla_draft_workspace_bytes, which also serves every step of fewer requests, fewer drafts or a narrower table
+ * With an 8-bit cache the latent values are what the codes stand for; computation is as exact as over a 16-bit cache.
+ * B * S <= TYPHOON_MLA_MAX_DRAFT_ROWS; tcgen05 kernel path only (UNSUPPORTED_DIMS otherwise); streams, capture and errors as
+ * typhoon_mla_decode.
+ */
+#define TYPHOON_MLA_MAX_DRAFT_ROWS (1 << 20)
+int typhoon_mla_decode_draft(const typhoon_mla_shared_t* shared, const void* q_nope, const void* q_pe, int32_t B, int32_t S,
+                             const typhoon_mla_cache_t* cache /* host */, const int32_t* block_table, int32_t max_pages,
+                             const int32_t* seq_lens, const int32_t* draft_lens, const uint64_t* tree_mask, float softmax_scale,
+                             int32_t mode, void* out, float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of scratch typhoon_mla_decode_draft needs in `mode` (AUTO: either).  Host, pure; 0 on invalid arguments. */
+size_t typhoon_mla_draft_workspace_bytes(const typhoon_mla_shared_t* shared, int32_t B, int32_t S, int32_t max_pages, int32_t page_size,
+                                         int32_t mode);
+
+/*
  * Device-side checks.  The handle owns one status word in device memory, zero after
  * typhoon_mla_prepare_shared.  Kernels never trap or assert; instead they OR a bit into the word:
  *   TYPHOON_MLA_STATUS_WAIT_EXPIRED  a bounded in-kernel wait ran out (every wait on a copy or a tensor-core

@@ -75,6 +75,10 @@ def _load():
     lib.typhoon_mla_cache_append.argtypes = [C.POINTER(Cache), vp, i64, vp, i64, C.POINTER(Rope), vp, vp, i64, vp, vp]
     lib.typhoon_mla_cache_read.restype = C.c_int
     lib.typhoon_mla_cache_read.argtypes = [C.POINTER(Cache), vp, i64, vp, i64, vp, i64, vp, vp]
+    lib.typhoon_mla_draft_workspace_bytes.restype = sz
+    lib.typhoon_mla_draft_workspace_bytes.argtypes = [vp, i32, i32, i32, i32, i32]
+    lib.typhoon_mla_decode_draft.restype = C.c_int
+    lib.typhoon_mla_decode_draft.argtypes = [vp, vp, vp, i32, i32, C.POINTER(Cache), vp, i32, vp, vp, vp, f32, i32, vp, vp, vp, sz, vp]
     lib.typhoon_mla_host_range_mapped.restype = C.c_int
     lib.typhoon_mla_host_range_mapped.argtypes = [vp, i64]
     lib.typhoon_mla_naive_plan_multi.restype = C.c_int
@@ -466,6 +470,33 @@ def typhoon_mla_cache_read(cache: PagedCache, slots: torch.Tensor, ckv_out: Opti
         None if status is None else _need(status, "status", torch.int32, (1,), dev), torch._C._cuda_getCurrentRawStream(dev))
     _check(st, "typhoon_mla_cache_read")
     return ckv_out, kpe_out
+
+
+def typhoon_mla_draft_workspace_bytes(shared: SharedPrefix, B: int, S: int, max_pages: int, page_size: int, mode: int = MODE_AUTO) -> int:
+    return int(_lib.typhoon_mla_draft_workspace_bytes(shared.handle, B, S, max_pages, page_size, mode))
+
+
+def typhoon_mla_decode_draft(shared: SharedPrefix, q_nope, q_pe, cache: PagedCache, block_table, seq_lens, softmax_scale: float, out,
+                             workspace, tree_mask=None, draft_lens=None, mode: int = MODE_AUTO, lse_out=None) -> None:
+    """S drafted tokens for each of B requests (block_table int32 [B, max_pages], seq_lens int32 [B]; S = rows of q_nope / B):
+    q_nope [B * S, H, 128], q_pe [B * S, H, 64], out [B * S, H, 128] bf16, lse_out float32 [B * S, H]; tree_mask int64 [B, S] (bit i:
+    draft i is visible; None: a chain), draft_lens int32 [B]."""
+    B, max_pages = _sizes(block_table, 2, "block_table")
+    rows, H, _ = _sizes(q_nope, 3, "q_nope")
+    S = rows // B if B else 0
+    dev, bf, i32 = _device(), torch.bfloat16, torch.int32
+    if rows != B * S or H != shared.dims.num_heads:
+        raise ValueError(f"q_nope must hold the same number of rows for each of {B} requests, of {shared.dims.num_heads} heads; got {tuple(q_nope.shape)}")
+    if not workspace.is_cuda or workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous, on the current CUDA device ({dev})")
+    st = _lib.typhoon_mla_decode_draft(
+        shared.handle, _need(q_nope, "q_nope", bf, (rows, H, 128), dev), _need(q_pe, "q_pe", bf, (rows, H, 64), dev), B, S, cache.on(dev),
+        _need(block_table, "block_table", i32, (B, max_pages), dev), max_pages, _need(seq_lens, "seq_lens", i32, (B,), dev),
+        None if draft_lens is None else _need(draft_lens, "draft_lens", i32, (B,), dev),
+        None if tree_mask is None else _need(tree_mask, "tree_mask", torch.int64, (B, S), dev), softmax_scale, mode,
+        _need(out, "out", bf, (rows, H, 128), dev), None if lse_out is None else _need(lse_out, "lse_out", torch.float32, (rows, H), dev),
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), torch._C._cuda_getCurrentRawStream(dev))
+    _check(st, "typhoon_mla_decode_draft")
 
 
 def typhoon_mla_host_staging_bytes(shared: SharedPrefix, B: int, max_pages: int) -> int:

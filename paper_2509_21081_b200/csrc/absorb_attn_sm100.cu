@@ -665,7 +665,7 @@ cudaError_t launch_absorb_attn_sm100(const AbsorbAttn& a, const CUtensorMap* tm_
     p.desc = reinterpret_cast<const int4*>(a.desc);
     p.scale_log2 = a.scale * kLog2e;
     p.o_part = a.o_part; p.lse_part = a.lse_part; p.status = status;
-    p.o_lat_direct = n_chunks == 1 ? reinterpret_cast<__nv_bfloat16*>(o_lat_direct) : nullptr;
+    p.o_lat_direct = n_chunks == 1 && !a.partial_only ? reinterpret_cast<__nv_bfloat16*>(o_lat_direct) : nullptr;
     p.lse_direct = lse_direct;
     const int smem = kAbsorbSmem;
     dim3 grid(a.n_shared_chunks * p.shared_groups + a.n_suffix_chunks * head_groups * a.B, 1, 1);

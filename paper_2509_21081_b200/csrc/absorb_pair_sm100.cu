@@ -610,7 +610,7 @@ cudaError_t launch_absorb_pair_sm100(const AbsorbAttn& a, int64_t Ls_pad, void* 
     }
     if (a.n_shared_chunks == 0) { tm_ckv_sh = tm_ckv_pg; tm_kpe_sh = tm_kpe_pg; }
     if (a.n_suffix_chunks == 0) { tm_ckv_pg = tm_ckv_sh; tm_kpe_pg = tm_kpe_sh; }
-    const bool direct = n_chunks == 1;
+    const bool direct = n_chunks == 1 && !a.partial_only;
     const void* o = direct ? o_lat_direct : a.o_part;
     cudaError_t e = make_out_tmap(&tm_o_sf, o, !direct, a.H, a.B, n_chunks);
     if (e == cudaSuccess && a.stacked) e = make_out_tmap(&tm_o_sh, o, !direct, rows, 1, n_chunks);

@@ -139,7 +139,8 @@ struct Plan {
     int n_split_naive;       // KV splits of the warp-MMA naive kernel / tile ranges of the tcgen05 one
     int n_slots_naive;       // partial slots the naive kernel writes (>= n_split_naive)
     bool absorb_pairs;       // absorb attention by the kernel of 128 rows per CTA pair
-    int chunk;               // tokens per absorb chunk
+    int chunk;               // tokens per absorb chunk (of a step of drafted tokens: over the prefix)
+    int draft_chunk;         // tokens per suffix chunk of a step of drafted tokens
     int n_shared_chunks;     // absorb chunks over the shared prefix (ABSORB mode)
     int n_suffix_chunks;
     // byte offsets into the workspace
@@ -345,6 +346,58 @@ size_t query_bytes(const typhoon_mla_shared* sh, int B, int max_pages, int page_
                     worst = std::max(worst, make_plan(sh, tc, schedule, B, pages, page_size, m, -1, stacked).total);
     }
     return worst + 256;
+}
+
+// A step of S drafted tokens for each of B requests: the shared prefix as in a step of B * S requests (either form), the suffixes by the
+// kernel of 128 query rows per CTA pair, S * H rows per request.  The plan keeps within the floor of its sizes throughout, so the floor
+// is what a workspace has to hold, and one sized for a batch, a number of drafts and a table serves every smaller step.
+Plan draft_floor(const typhoon_mla_shared* sh, int B, int S, int max_pages, int page_size, int mode) {
+    const int H = sh->dims.num_heads, n_sm = sh->num_sms > 0 ? sh->num_sms : kDefaultNumSM;
+    const int64_t rows = (int64_t)B * S * H, cap = (int64_t)max_pages * page_size;
+    const bool absorb_prefix = mode == TYPHOON_MLA_MODE_ABSORB;
+    Plan p{};
+    lay_out(&p, B * S, H, floor_chunk_rows(n_sm, rows, absorb_prefix ? sh->Ls : 0, cap), absorb_prefix ? 0 : floor_slot_rows(n_sm, rows, sh->Ls));
+    return p;
+}
+Plan make_draft_plan(const typhoon_mla_shared* sh, int schedule, bool stacked, int B, int S, int max_pages, int page_size, int mode) {
+    const int H = sh->dims.num_heads, n_sm = sh->num_sms > 0 ? sh->num_sms : kDefaultNumSM, Q = B * S;
+    const int64_t rows = (int64_t)Q * H, cap = (int64_t)max_pages * page_size;
+    const int64_t Ls_absorb = mode == TYPHOON_MLA_MODE_ABSORB ? sh->Ls : 0;
+    const int row_tiles = (S * H + 127) / 128;
+    const int64_t tiles = (cap + 127) / 128;
+    Plan p{};
+    p.mode = mode;
+    if (mode != TYPHOON_MLA_MODE_ABSORB && sh->Ls > 0) {
+        // SM time of the absorb branch beside it (as absorb_branch_us, with row_tiles items per request)
+        const double beside = 4.0 * H * ((Q + 127) / 128) + 2.0 * B * row_tiles * (10.0 + 1.25 * (double)tiles);
+        const int max_slots = (int)std::min<int64_t>(floor_slot_rows(n_sm, rows, sh->Ls) / rows, INT32_MAX);
+        naive_sm100_plan(Q, H, sh->Ls, naive_places(Q, n_sm, sh->fp8 != 0), schedule, &p.n_split_naive, &p.n_slots_naive, sh->fp8 != 0, beside,
+                         max_slots);
+    }
+    int max_chunks = (int)std::min<int64_t>(floor_chunk_rows(n_sm, rows, Ls_absorb, cap) / rows, kMaxAbsorbChunks);
+    if (Ls_absorb > 0) {
+        int none = 0;
+        absorb_chunks(true, stacked, false, n_sm, Q, H, Ls_absorb, 0, max_chunks - 1, &p.absorb_pairs, &p.chunk, &p.n_shared_chunks, &none);
+        max_chunks -= p.n_shared_chunks;
+    }
+    // the suffix: waves x (tiles per chunk + fixed cost in tiles), with the pair kernel's constants (absorb_chunks)
+    double best = 1e30;
+    int64_t weighed = 0;
+    for (int parts = 1; parts <= max_chunks; ++parts) {
+        const int64_t ch = round_up((cap + parts - 1) / parts, 128);
+        if (ch == weighed) continue;
+        weighed = ch;
+        const int64_t n = (cap + ch - 1) / ch, waves = (n * B * row_tiles + n_sm / 2 - 1) / (n_sm / 2);
+        const double cost = (double)waves * ((double)ch / 128 + 4.0 + (n + p.n_shared_chunks > 1 ? 3.0 : 0.0));
+        if (cost < best - 1e-9) {
+            best = cost;
+            p.draft_chunk = (int)ch;
+            p.n_suffix_chunks = (int)n;
+        }
+        if (ch <= 128) break;
+    }
+    lay_out(&p, Q, H, (int64_t)(p.n_shared_chunks + p.n_suffix_chunks) * rows, (int64_t)p.n_slots_naive * rows);
+    return p;
 }
 
 // The handle's buffers, stream and events live on the device it was prepared on.
@@ -605,6 +658,7 @@ static int prepare_impl(const typhoon_mla_dims_t* dims, const void* ckv_shared, 
     if (e == cudaSuccess) e = set_attrs_naive_pair_sm100();
     if (e == cudaSuccess) e = set_attrs_absorb_sm100();
     if (e == cudaSuccess) e = set_attrs_absorb_pair_sm100();
+    if (e == cudaSuccess) e = set_attrs_draft_sm100();
     if (e == cudaSuccess) e = set_attrs_expand_sm100();
     if (e == cudaSuccess) e = set_attrs_project_sm100();
     if (e == cudaSuccess) e = set_attrs_q_absorb_sm100();
@@ -883,6 +937,14 @@ struct EmptySlots {
     int slot0, n_slots, row0, rows;
 };
 
+// A step of drafted tokens: the suffixes of n_requests requests of S query tokens each, in place of B requests of one.
+struct DraftStep {
+    const typhoon_mla_cache_t* cache;
+    int n_requests, S;
+    const int32_t* draft_lens;
+    const uint64_t* mask;
+};
+
 // Launch sequence of one step.  `sh` provides the weights, the absorb-side tensor maps, the side stream
 // and the status word; `mode` is resolved (ABSORB, HYBRID or NAIVE); `pl.n_slots_naive` is the total
 // number of naive partial slots.
@@ -892,7 +954,7 @@ static int decode_core(const Settings& cfg, const typhoon_mla_shared* sh, const 
                 const Plan& pl, const void* q_nope, const void* q_pe, int32_t B, const void* ckv_pages,
                 const void* kpe_pages, int64_t ckv_token_stride, int64_t kpe_token_stride, int32_t page_size, int32_t num_pages,
                 const int32_t* block_table, int32_t max_pages, const int32_t* seq_lens, float softmax_scale, int32_t mode,
-                void* out, float* lse_out, void* workspace, void* stream, bool out_fp32 = false) {
+                void* out, float* lse_out, void* workspace, void* stream, bool out_fp32 = false, const DraftStep* draft = nullptr) {
     const bool use_absorb = mode != TYPHOON_MLA_MODE_NAIVE;
     tmla::tl_pdl = cfg.pdl;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
@@ -974,7 +1036,8 @@ static int decode_core(const Settings& cfg, const typhoon_mla_shared* sh, const 
         // sync): by an extra block of the query-absorption kernel on the tcgen05 path, by its own kernel otherwise
         int32_t* order = nullptr;
         int32_t* desc = nullptr;   // per-position descriptors, written next to the order on the tcgen05 path
-        if (pl.n_suffix_chunks > 0 && B > 1 && B <= 4096) order = reinterpret_cast<int32_t*>(ws + pl.off_order);
+        const int n_requests = draft ? draft->n_requests : B;
+        if (pl.n_suffix_chunks > 0 && n_requests > 1 && n_requests <= 4096) order = reinterpret_cast<int32_t*>(ws + pl.off_order);
         // --- query absorption Q_A = Q_N W_UK (Algorithm 1 line 5)
         void* q_abs = ws + pl.off_qabs;
         prof_before(TYPHOON_MLA_KERNEL_Q_ABSORB, s);
@@ -1004,7 +1067,7 @@ static int decode_core(const Settings& cfg, const typhoon_mla_shared* sh, const 
                 }
             }
             e = launch_q_absorb_sm100(q_nope, &sh->tm_wuk_t, q_abs, B, H, sh->num_sms, walk_ctas, sh->status, order ? seq_lens : nullptr, order,
-                                      block_table, max_pages, page_size, desc, s);
+                                      block_table, max_pages, page_size, desc, s, n_requests);
         } else {
             GemmTN g1{q_nope, (int64_t)H * 128, 128, sh->w_uk_t, 128, 512 * 128, q_abs, (int64_t)H * 512, 512,
                       B, 512, 128, H, false};
@@ -1023,12 +1086,20 @@ static int decode_core(const Settings& cfg, const typhoon_mla_shared* sh, const 
         void* o_lat = ws + pl.off_olat;
         AbsorbAttn ab{q_abs, q_pe, sh->ckv, sh->kpe, mode == TYPHOON_MLA_MODE_ABSORB ? (int)sh->Ls : 0,
                       ckv_pages, kpe_pages, ckv_token_stride, kpe_token_stride, page_size, num_pages, block_table, max_pages,
-                      seq_lens, order, desc, B, H, pl.chunk, pl.n_shared_chunks, pl.n_suffix_chunks, softmax_scale,
-                      o_part_a, lse_part_a, sh->status, forked ? nullptr : sh->w_uv, cfg.stacked_absorb};
+                      seq_lens, order, desc, B, H, pl.chunk, pl.n_shared_chunks, draft ? 0 : pl.n_suffix_chunks, softmax_scale,
+                      o_part_a, lse_part_a, sh->status, forked ? nullptr : sh->w_uv, draft != nullptr, cfg.stacked_absorb};
         prof_before(TYPHOON_MLA_KERNEL_ABSORB_ATTN, s);
-        if (!tc) e = launch_absorb_attn_mma(ab, s);
+        if (draft && pl.n_shared_chunks == 0) e = cudaSuccess;   // (the suffix is the kernel's below)
+        else if (!tc) e = launch_absorb_attn_mma(ab, s);
         else if (pl.absorb_pairs) e = launch_absorb_pair_sm100(ab, sh->Ls_pad, o_lat, lse_a, sh->status, s);
         else e = launch_absorb_attn_sm100(ab, &sh->tm_ckv, &sh->tm_kpe_tok, o_lat, lse_a, sh->status, s);
+        if (draft && e == cudaSuccess) {
+            if (pl.n_shared_chunks > 0) ++launches;
+            const DraftAttn da{q_abs, q_pe, draft->cache, block_table, max_pages, seq_lens, draft->draft_lens, draft->mask, desc, draft->n_requests,
+                               draft->S, H, pl.draft_chunk, pl.n_suffix_chunks, pl.n_shared_chunks, softmax_scale, o_part_a, lse_part_a,
+                               forked ? nullptr : sh->w_uv};
+            e = launch_draft_sm100(da, n_chunks == 1 ? o_lat : nullptr, lse_a, sh->status, s);
+        }
         prof_after(TYPHOON_MLA_KERNEL_ABSORB_ATTN, s);
         if (e != cudaSuccess) return fail(e);
         ++launches;
@@ -1158,6 +1229,50 @@ int typhoon_mla_combine_partials(const float* o_parts, const float* lse_parts, i
     if (e != cudaSuccess) return cuda_fail(e);
     g_last_launches = 1;
     return TYPHOON_MLA_OK;
+}
+// ---- drafted tokens ---------------------------------------------------------------------------------
+static bool draft_sizes_valid(const typhoon_mla_shared_t* sh, int32_t B, int32_t S, int32_t max_pages, int32_t mode) {
+    return sh && B >= 1 && S >= 1 && S <= 64 && (int64_t)B * S <= TYPHOON_MLA_MAX_DRAFT_ROWS && max_pages >= 1 && max_pages <= (1 << 24) &&
+           mode >= TYPHOON_MLA_MODE_AUTO && mode <= TYPHOON_MLA_MODE_HYBRID;
+}
+
+size_t typhoon_mla_draft_workspace_bytes(const typhoon_mla_shared_t* sh, int32_t B, int32_t S, int32_t max_pages, int32_t page_size,
+                                         int32_t mode) {
+    if (!draft_sizes_valid(sh, B, S, max_pages, mode) || (page_size != 64 && page_size != 128)) return 0;
+    // (a step of single tokens over a 16-bit cache is typhoon_mla_decode's)
+    size_t worst = query_bytes(sh, B * S, max_pages, page_size, mode);
+    for (int m : {TYPHOON_MLA_MODE_ABSORB, TYPHOON_MLA_MODE_HYBRID})
+        if (mode == TYPHOON_MLA_MODE_AUTO || mode == m || sh->Ls == 0) worst = std::max(worst, draft_floor(sh, B, S, max_pages, page_size, m).total);
+    return worst + 256;
+}
+
+int typhoon_mla_decode_draft(const typhoon_mla_shared_t* sh, const void* q_nope, const void* q_pe, int32_t B, int32_t S,
+                             const typhoon_mla_cache_t* cache, const int32_t* block_table, int32_t max_pages, const int32_t* seq_lens,
+                             const int32_t* draft_lens, const uint64_t* tree_mask, float softmax_scale, int32_t mode, void* out,
+                             float* lse_out, void* workspace, size_t workspace_bytes, void* stream) {
+    g_last_launches = 0;
+    if (!draft_sizes_valid(sh, B, S, max_pages, mode) || !cache_valid(cache)) return TYPHOON_MLA_ERR_INVALID_ARG;
+    if (!q_nope || !q_pe || !out || !block_table || !seq_lens) return TYPHOON_MLA_ERR_INVALID_ARG;
+    if (!on_handle_device(sh)) return TYPHOON_MLA_ERR_INVALID_ARG;
+    if (!aligned16(q_nope) || !aligned16(q_pe) || !aligned16(out) || (reinterpret_cast<uintptr_t>(tree_mask) & 7u)) return TYPHOON_MLA_ERR_INVALID_ARG;
+    if (!(softmax_scale > 0.f) || softmax_scale > 3.0e38f) return TYPHOON_MLA_ERR_INVALID_ARG;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return TYPHOON_MLA_ERR_INVALID_ARG;
+    const Settings cfg = snapshot();
+    if (!cfg.tc()) return TYPHOON_MLA_ERR_UNSUPPORTED_DIMS;
+    const int page_size = cache->page_size;
+    if (S == 1 && !draft_lens && !tree_mask && !cache->ckv_exponents)   // single tokens, each of which sees everything
+        return decode_impl(sh, q_nope, q_pe, B, cache->ckv_pages, cache->kpe_pages, cache->ckv_token_stride, cache->kpe_token_stride, page_size,
+                           cache->num_pages, block_table, max_pages, seq_lens, softmax_scale, mode, out, lse_out, workspace, workspace_bytes,
+                           stream, false);
+    const int rows = B * S;
+    mode = resolve_mode(sh, rows, max_pages, mode);
+    const Plan pl = make_draft_plan(sh, cfg.naive_schedule, cfg.stacked_absorb, B, S, max_pages, page_size, mode);
+    if (workspace_bytes < pl.total) return TYPHOON_MLA_ERR_WORKSPACE_TOO_SMALL;
+    const DraftStep draft{cache, B, S, draft_lens, tree_mask};
+    NaiveJob job{sh, 0, rows, pl.n_split_naive, pl.n_slots_naive, 0};
+    return decode_core(cfg, sh, &job, pl.n_split_naive > 0 ? 1 : 0, nullptr, 0, pl, q_nope, q_pe, rows, cache->ckv_pages, cache->kpe_pages,
+                       cache->ckv_token_stride, cache->kpe_token_stride, page_size, cache->num_pages, block_table, max_pages, seq_lens,
+                       softmax_scale, mode, out, lse_out, workspace, stream, false, &draft);
 }
 // ---- several shared prefixes per step (tree-structured prompts) ------------------------------------
 namespace {

@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(512, 1) merge_project_kernel(const float* __re
         if (out_fp32) reinterpret_cast<float*>(out)[idx] = res;
         else reinterpret_cast<__nv_bfloat16*>(out)[idx] = __float2bfloat16_rn(res);
     }
-    if (tid == 0 && lse_out != nullptr) lse_out[bh] = (m == -INFINITY) ? -INFINITY : m + __logf(z);
+    if (tid == 0 && lse_out != nullptr) lse_out[bh] = (m == -INFINITY) ? -INFINITY : merged_lse(m, z);
 }
 
 // One warp per (b, h); each lane owns 4 of the 128 output columns.

@@ -14,6 +14,12 @@ constexpr int kDl = 512;   // D_l  latent width
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// LSE by which a partial of drafted tokens says that some logit of the row is not finite: its weight in any merge is 1 and its values
+// are NaN, so the row becomes NaN.
+constexpr float kLseNotFinite = 3.2e38f;
+// LSE of a row from the largest of its partials' and the sum of their weights (m > -inf).
+__device__ __forceinline__ float merged_lse(float m, float z) { return m < kLseNotFinite ? m + __logf(z) : __int_as_float(0x7fc00000); }
+
 __device__ __forceinline__ uint32_t smem_u32(const void* p) {
     return static_cast<uint32_t>(__cvta_generic_to_shared(p));
 }

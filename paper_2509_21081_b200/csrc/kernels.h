@@ -28,6 +28,7 @@ cudaError_t set_attrs_naive_sm100();
 cudaError_t set_attrs_naive_pair_sm100();
 cudaError_t set_attrs_absorb_sm100();
 cudaError_t set_attrs_absorb_pair_sm100();
+cudaError_t set_attrs_draft_sm100();
 cudaError_t set_attrs_expand_sm100();
 cudaError_t set_attrs_project_sm100();
 cudaError_t set_attrs_q_absorb_sm100();
@@ -108,11 +109,12 @@ cudaError_t make_q_absorb_tmap(const void* w_uk_t, int H, CUtensorMap* tm_w);
 // With seq_lens and order given (B <= 4096) one extra block also writes the longest-first request order and,
 // with desc given, one int4 per launch position {request, clamped suffix length, first page, second page}
 // (-1 where the block table has no such column) that saves the absorb kernel three dependent loads.
+// n_requests > 0: that many requests have lengths and table rows, fewer than the B query rows.
 // walk_ctas > 0 (and B <= 128): that many CTAs walk through the heads instead of one CTA per head (for launches that share the
 // GPU with a kernel that leaves only a few SMs free).
 cudaError_t launch_q_absorb_sm100(const void* q_nope, const CUtensorMap* tm_w, void* q_abs, int B, int H, int n_sm, int walk_ctas, int* status,
                                   const int32_t* seq_lens, int32_t* order, const int32_t* block_table, int max_pages,
-                                  int page_size, int32_t* desc, cudaStream_t s);
+                                  int page_size, int32_t* desc, cudaStream_t s, int n_requests = 0);
 
 // Naive shared-prefix attention partials (Algorithm 1 line 4).
 struct NaiveAttn {
@@ -199,6 +201,7 @@ struct AbsorbAttn {
     float* lse_part; // [n_chunks][B][H]
     int* status = nullptr;   // device word: bit 0x100 is set when a page id was out of range
     const void* w_uv = nullptr;   // optional, 16-byte aligned [H][128][512] bf16: requested into L2 for the kernel that follows
+    bool partial_only = false;   // tcgen05 kernels: partials even with a single chunk (another launch adds chunks of its own)
     bool stacked = false;    // tcgen05 kernel: shared-prefix chunks take 64-row groups of the stacked [B*H] queries
 };
 cudaError_t launch_absorb_attn_mma(const AbsorbAttn& p, cudaStream_t s);
@@ -215,6 +218,24 @@ cudaError_t make_absorb_shared_tmaps(const void* ckv, const void* kpe, int64_t L
 // The same for 128 query rows per pair of CTAs and at most 128 heads (chunk must be a multiple of 128).
 cudaError_t launch_absorb_pair_sm100(const AbsorbAttn& a, int64_t Ls_pad, void* o_lat_direct, float* lse_direct, int* status,
                                      cudaStream_t s);
+
+// Absorb attention of drafted tokens over the paged cache (16- or 8-bit), S query tokens per request, chunk a multiple of 128.
+// Partials go to slots [chunk0, chunk0 + n_chunks) of o_part / lse_part, or, with o_lat_direct (a single chunk in all), the merged
+// bf16 latent output [B * S, H, 512] and its LSE there.
+struct DraftAttn {
+    const void* q_abs; const void* q_pe;           // [B*S,H,512], [B*S,H,64]
+    const typhoon_mla_cache_t* cache;
+    const int32_t* block_table; int max_pages; const int32_t* seq_lens;
+    const int32_t* draft_lens;                     // optional [B]: how many of the suffix's last tokens are drafts (else S)
+    const uint64_t* mask;                          // optional [B,S]: bit i, draft i is visible to the row (else 0 .. j to row j)
+    const int32_t* desc;                           // optional [B][4]: per launch position, see launch_q_absorb_sm100
+    int B, S, H; int chunk, n_chunks, chunk0;
+    float scale;
+    float* o_part;   // [slots][B*S][H][512], each normalised
+    float* lse_part; // [slots][B*S][H]
+    const void* w_uv = nullptr;                    // as in AbsorbAttn
+};
+cudaError_t launch_draft_sm100(const DraftAttn& a, void* o_lat_direct, float* lse_direct, int* status, cudaStream_t s);
 
 // perm[0..B) = request indices by descending suffix length (B <= 4096).
 // -inf into n_slots segments of `count` floats, `stride` floats apart.

@@ -260,7 +260,7 @@ project_sm100_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
                 if (!live) continue;
                 store_row32(ce, bh * 128 + it.n0 + c * 32, acc + c * 32, t, wa, inv);
             }
-            if (live && it.n0 == 0 && ce.lse_out) ce.lse_out[bh] = (m == -INFINITY) ? -INFINITY : m + __logf(zsum);
+            if (live && it.n0 == 0 && ce.lse_out) ce.lse_out[bh] = (m == -INFINITY) ? -INFINITY : merged_lse(m, zsum);
         }
     }
     tc_fence_before();
@@ -369,7 +369,7 @@ project_latency_sm100_kernel(const __grid_constant__ CUtensorMap tmA, const __gr
             wn = (ln == -INFINITY) ? 0.f : __expf(ln - m);      // (an empty partial's slot was never written)
             const float z = wa + wn;
             inv = z > 0.f ? 1.f / z : 0.f;
-            if (m != -INFINITY) lse = m + __logf(z);
+            if (m != -INFINITY) lse = merged_lse(m, z);
         }
         const float4* src = reinterpret_cast<const float4*>(ce.o_naive + bh * 128 + n0);
 #pragma unroll

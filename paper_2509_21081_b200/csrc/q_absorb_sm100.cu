@@ -42,6 +42,7 @@ struct QAbsorbParams {
     // absorb attention kernel launched next uses, saving a launch on the absorb branch
     const int32_t* seq_lens;
     int32_t* order;
+    int n_requests;
     // optional per-position descriptors for the absorb kernel
     const int32_t* block_table;
     int max_pages, page_size;
@@ -58,10 +59,10 @@ q_absorb_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
     if (walk ? (int)blockIdx.x == p.walk_ctas : (int)blockIdx.y == p.H) {   // the ordering block (whole block takes this branch)
         pdl_wait();
         if (walk || blockIdx.x == 0) {
-            block_order_by_length(p.seq_lens, p.B, p.order, reinterpret_cast<unsigned long long*>(smem));
+            block_order_by_length(p.seq_lens, p.n_requests, p.order, reinterpret_cast<unsigned long long*>(smem));
             if (p.desc != nullptr) {
                 __syncthreads();   // perm[] written by this block is read back below
-                for (int i = threadIdx.x; i < p.B; i += blockDim.x) {
+                for (int i = threadIdx.x; i < p.n_requests; i += blockDim.x) {
                     const int b = p.order[i];
                     const int len = min(max(p.seq_lens[b], 0), p.max_pages * p.page_size);
                     const int32_t* bt = p.block_table + (int64_t)b * p.max_pages;
@@ -266,8 +267,9 @@ cudaError_t make_q_absorb_tmap(const void* w_uk_t, int H, CUtensorMap* tm_w) {
 
 cudaError_t launch_q_absorb_sm100(const void* q_nope, const CUtensorMap* tm_w, void* q_abs, int B, int H, int n_sm, int walk_ctas, int* status,
                                   const int32_t* seq_lens, int32_t* order, const int32_t* block_table, int max_pages,
-                                  int page_size, int32_t* desc, cudaStream_t s) {
+                                  int page_size, int32_t* desc, cudaStream_t s, int n_requests) {
     if (B <= 0) return cudaSuccess;
+    if (n_requests <= 0) n_requests = B;
     CUtensorMap tm_q, tm_out;
     {
         uint64_t dims[3] = {128, (uint64_t)H, (uint64_t)B};
@@ -283,14 +285,14 @@ cudaError_t launch_q_absorb_sm100(const void* q_nope, const CUtensorMap* tm_w, v
         cudaError_t e = make_tmap_bf16(&tm_out, q_abs, 3, dims, str, box);
         if (e != cudaSuccess) return e;
     }
-    const bool with_order = seq_lens != nullptr && order != nullptr && B <= 4096;
+    const bool with_order = seq_lens != nullptr && order != nullptr && n_requests <= 4096;
     const int n_tiles = (B + 127) / 128;
     // one CTA per head keeps the head's weights resident over all of its request tiles; with more SMs than heads
     // the tiles of a head are dealt to several CTAs
     const int splits = std::max(1, std::min(n_tiles, std::max(n_sm, 1) / H));
     // walk mode only with one request tile per head and fewer working CTAs than heads
     const int walk = (n_tiles == 1 && walk_ctas > 0 && walk_ctas < H) ? walk_ctas : 0;
-    QAbsorbParams p{q_abs, B, H, n_tiles, splits, walk, status, seq_lens, order, block_table, max_pages, page_size,
+    QAbsorbParams p{q_abs, B, H, n_tiles, splits, walk, status, seq_lens, order, n_requests, block_table, max_pages, page_size,
                     (with_order && block_table != nullptr) ? reinterpret_cast<int4*>(desc) : nullptr};
     const dim3 grid = walk ? dim3(walk + (with_order ? 1 : 0), 1, 1) : dim3(splits, H + (with_order ? 1 : 0), 1);
     return launch_pdl(q_absorb_sm100_kernel, grid, dim3(192), B <= DIRECT_ROWS ? SMEM_BYTES_DIRECT : SMEM_BYTES, s, tm_q, *tm_w, tm_out, p);
