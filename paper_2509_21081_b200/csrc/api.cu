@@ -1040,6 +1040,8 @@ static int decode_core(const Settings& cfg, const typhoon_mla_shared* sh, const 
         if (pl.n_suffix_chunks > 0 && n_requests > 1 && n_requests <= 4096) order = reinterpret_cast<int32_t*>(ws + pl.off_order);
         // --- query absorption Q_A = Q_N W_UK (Algorithm 1 line 5)
         void* q_abs = ws + pl.off_qabs;
+        void* q_terms = nullptr;
+        float* q_tau = nullptr;
         prof_before(TYPHOON_MLA_KERNEL_Q_ABSORB, s);
         if (tc) {
             if (order) desc = reinterpret_cast<int32_t*>(ws + pl.off_desc);
@@ -1066,8 +1068,14 @@ static int decode_core(const Settings& cfg, const typhoon_mla_shared* sh, const 
                     if ((double)tiles_per_cta * tile_us >= 4.0 * heads_per_cta) walk_ctas = free_sms;
                 }
             }
-            e = launch_q_absorb_sm100(q_nope, &sh->tm_wuk_t, q_abs, B, H, sh->num_sms, walk_ctas, sh->status, order ? seq_lens : nullptr, order,
-                                      block_table, max_pages, page_size, desc, s, n_requests);
+            // An 8-bit cache takes the absorbed queries as E4M3 terms.  Where the prefix is attended in absorb form as well, that takes the
+            // bf16 rows, and the terms go where the merge behind both will put the latent output.
+            if (draft && draft->cache->ckv_exponents) {
+                q_terms = pl.n_shared_chunks > 0 ? ws + pl.off_olat : q_abs;
+                q_tau = o_abs;   // (the warp-MMA path's)
+            }
+            e = launch_q_absorb_sm100(q_nope, &sh->tm_wuk_t, q_terms == q_abs ? nullptr : q_abs, B, H, sh->num_sms, walk_ctas, sh->status, order ? seq_lens : nullptr, order,
+                                      block_table, max_pages, page_size, desc, s, n_requests, q_terms, q_tau);
         } else {
             GemmTN g1{q_nope, (int64_t)H * 128, 128, sh->w_uk_t, 128, 512 * 128, q_abs, (int64_t)H * 512, 512,
                       B, 512, 128, H, false};
@@ -1095,7 +1103,7 @@ static int decode_core(const Settings& cfg, const typhoon_mla_shared* sh, const 
         else e = launch_absorb_attn_sm100(ab, &sh->tm_ckv, &sh->tm_kpe_tok, o_lat, lse_a, sh->status, s);
         if (draft && e == cudaSuccess) {
             if (pl.n_shared_chunks > 0) ++launches;
-            const DraftAttn da{q_abs, q_pe, draft->cache, block_table, max_pages, seq_lens, draft->draft_lens, draft->mask, desc, draft->n_requests,
+            const DraftAttn da{q_terms ? q_terms : q_abs, q_pe, q_tau, draft->cache, block_table, max_pages, seq_lens, draft->draft_lens, draft->mask, desc, draft->n_requests,
                                draft->S, H, pl.draft_chunk, pl.n_suffix_chunks, pl.n_shared_chunks, softmax_scale, o_part_a, lse_part_a,
                                forked ? nullptr : sh->w_uv};
             e = launch_draft_sm100(da, n_chunks == 1 ? o_lat : nullptr, lse_a, sh->status, s);

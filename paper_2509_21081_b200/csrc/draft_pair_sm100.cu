@@ -14,19 +14,21 @@
 // sees nothing in a chunk gets weight zero there.
 //
 // 8-bit latent rows.  Widening codes to 16 bits on the way would take as much shared-memory traffic as the products themselves.
-// Instead the products run on the codes (kind::f8f6f4, twice the rate of 16 bits) and the 16-bit operand is split: a bf16 value has
-// 8 significant bits, so with m = its mantissa as an integer in [128, 256) the nearest multiple of 16 and the rest, at most 8, are
-// both E4M3 numbers: q = q1 + q2 exactly, and P = p1 + p2 to the same 8 bits.  Two products at twice the rate: the time, the
-// operand bytes and the rounding of the 16-bit kernel, on half the cache bytes.  What is left of the range: a row of Q is scaled by a
+// Instead the products run on the codes (kind::f8f6f4, twice the rate of 16 bits) and the other operand is split into two E4M3
+// numbers, the nearest one and the nearest one to the rest: 4 significant bits, a sign and 4 more, at least the 8 bits of bf16 (with
+// m = the mantissa of a bf16 value as an integer in [128, 256) the nearest multiple of 16 and the rest, at most 8, are both exact;
+// split from 32 bits the sum is off by 6e-4 of the value in the mean square, bf16 by 1.6e-3).  Two products at twice the rate: the
+// time and the operand bytes of the 16-bit kernel, on half the cache bytes.  What is left of the range: a row of Q is scaled by a
 // power of two to an amax in [224, 448], so an element loses bits only where it is 2^-10 of the row's largest (by 2^-18 of that at
 // most); P is held to at most 2^8 with 2^4 at the reference, so a weight is good to 2^-14 of the row's largest contribution.
 // The rope part (16-bit, unscaled) goes to an accumulator of its own, and a logit is S_lat * 2^(tau + e_t) + S_rope.  The token's power
 // of two belongs to its values as well: with x the scaled logit in log2 units, P = 2^(x + e_t - n) against a reference n of the
 // x + e_t, and the row sum is of 2^(x - m) against one of the x (per thread; any reference within 2^60 will do in 32 bits).
 //
+// (Query absorption splits Q, from 32 bits; the split of P is here, from 32 bits as well.)
+//
 // Warp roles (384 threads per CTA): warp 0 loads K tiles (and Q), warp 2 the second operand; warp 1 allocates tensor memory and in
-// the even CTA issues both products; warp 3 lays out the tokens' powers of two; warps 4-11 softmax and epilogue, and before that the
-// split of Q.
+// the even CTA issues both products; warp 3 lays out the tokens' powers of two; warps 4-11 softmax and epilogue.
 #include <algorithm>
 #include <cstddef>
 
@@ -58,7 +60,7 @@ struct DraftParams {
     __nv_bfloat16* o_lat_direct;   // single chunk: the merged result bf16 [B * rows][512], and its LSE
     float* lse_direct;
     int* status;
-    const __nv_bfloat16* q_abs;    // 8 bits: [B * rows][512]
+    const float* q_tau;            // 8 bits: power of two of a row of Q, [B * rows]
     const uint8_t* exponents;      // 8 bits: [num_pages][page_size]
     const char* l2_base;   // read by the kernel behind this one: requested into L2
     uint32_t l2_total, l2_bytes;
@@ -91,9 +93,10 @@ struct Shared {
     int abort_flag;
     float red[4][64];                 // [token quarter][row]
     float red2[E8 ? 4 : 1][E8 ? 64 : 1];
-    float tau[E8 ? 64 : 1];           // power of two of a row of Q
-    alignas(16) float sc[E8 ? 4 : 1][E8 ? TOK : 4];      // of a token ...
-    alignas(16) float lg[E8 ? 4 : 1][E8 ? TOK : 4];      // ... and its exponent
+    alignas(16) float sc[E8 ? 4 : 1][E8 ? TOK : 4];      // of a token (times the softmax scale) ...
+    alignas(16) float lg[E8 ? 4 : 1][E8 ? TOK : 4];      // ... its exponent
+    alignas(16) float isc[E8 ? 4 : 1][E8 ? TOK : 4];     // ... and its inverse
+    int wide[E8 ? 4 : 1];             // some token up to this tile has one outside 2^+-40
 };
 
 // (all of an SM's shared memory either way: no other kernel that allocates tensor memory fits beside a CTA)
@@ -116,25 +119,6 @@ __device__ __forceinline__ bool vote_or(bool pred) {   // over the 256 softmax t
     return r != 0;
 }
 __device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync %0, 256;\n" ::"n"(kSoftmaxBar) : "memory"); }
-
-// Two E4M3 codes (low byte: a) and what is left of the pair.
-__device__ __forceinline__ uint32_t e4m3_pair(float a, float b) {
-    uint16_t d;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(d) : "f"(b), "f"(a));
-    return d;
-}
-__device__ __forceinline__ float2 e4m3_values(uint32_t codes) {
-    uint32_t h2;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(h2) : "h"((uint16_t)codes));
-    return __half22float2(*reinterpret_cast<__half2*>(&h2));
-}
-// Four values as codes of their first and second term.
-__device__ __forceinline__ void split4(float a, float b, float c, float d, uint32_t& first, uint32_t& second) {
-    const uint32_t x = e4m3_pair(a, b), y = e4m3_pair(c, d);
-    const float2 u = e4m3_values(x), v = e4m3_values(y);
-    first = x | (y << 16);
-    second = e4m3_pair(a - u.x, b - u.y) | (e4m3_pair(c - v.x, d - v.y) << 16);
-}
 
 template <bool E8>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(384, 1)
@@ -160,7 +144,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
         uint64_t* all = &sh->q_full;
         constexpr int n_bars = (int)(offsetof(Shared<E8>, tmem_base) / sizeof(uint64_t));
         static_assert(n_bars <= 32, "one lane per barrier");
-        if (lane < n_bars) mbar_init(all + lane, all + lane == &sh->p_ready ? 16 : all + lane >= &sh->sc_empty[0] ? 8 : E8 && lane == 0 ? 17 : 1);
+        if (lane < n_bars) mbar_init(all + lane, all + lane == &sh->p_ready ? 16 : all + lane >= &sh->sc_empty[0] ? 8 : 1);
         if (lane == 0) sh->abort_flag = 0;
         fence_mbar_init();
         __syncwarp();
@@ -260,11 +244,9 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                 if (j == 0) {
                     const uint32_t qf = cluster_map(&sh->q_full, 0);
                     const int y = (int)row0 + 64 * (int)rank;
-                    mbar_arrive_expect_tx_if(ld_even, &sh->q_full, 2 * (E8 ? SLAB : X::Q_BYTES));
-                    if (!E8) {
+                    mbar_arrive_expect_tx_if(ld_even, &sh->q_full, 2 * X::Q_BYTES);
 #pragma unroll 1
-                        for (int sl = 0; sl < 8; ++sl) tma_load_2d_pair_if(ld, sQ + sl * SLAB, &tm_qa, qf, sl * 64, y);
-                    }
+                    for (int sl = 0; sl < 8; ++sl) tma_load_2d_pair_if(ld, sQ + sl * SLAB, &tm_qa, qf, sl * 64, y);
                     tma_load_2d_pair_if(ld, sQ + 8 * SLAB, &tm_qp, qf, 0, y);
                     for (int i = 1; i < KS + 1; ++i) prefetch_tile(i);
                 }
@@ -403,50 +385,15 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
             const int quarter = 2 * half + w;
             const uint32_t lane_base = (uint32_t)(32 * q) << 16;
             const uint32_t p_bar = cluster_map(&sh->p_ready, 0);
-            if (E8) {
-                // Q of this CTA's 64 rows as two E4M3 terms under a power of two per row; a warp takes 8 rows, 16 dims per lane
-#pragma unroll 2
-                for (int i = 0; i < 8; ++i) {
-                    const int r = 8 * (warp - 4) + i;
-                    uint32_t v[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = 0;
-                    if (64 * (int)rank + r < n_rows) {
-                        const uint4* src = reinterpret_cast<const uint4*>(p.q_abs + (row0 + 64 * (int)rank + r) * 512) + 2 * lane;
-                        const uint4 a = src[0], c = src[1];
-                        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = c.x; v[5] = c.y; v[6] = c.z; v[7] = c.w;
-                    }
-                    uint32_t m2 = 0;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) m2 = __vmaxu2(m2, v[e] & 0x7fff7fffu);
-                    const uint32_t m = __reduce_max_sync(0xffffffffu, max(m2 & 0xffffu, m2 >> 16));
-                    // exponent field of the power of two, as for a row of the cache (above 448 = 1.75 * 2^8); kept within 1 .. 246, where
-                    // it and its inverse are normal numbers
-                    const int byte = min(max((int)(m >> 7) - 8 + ((m & 0x7fu) > 0x60u ? 1 : 0), 1), 247);
-                    const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);
-                    uint32_t first[4], second[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        split4(__uint_as_float(v[2 * e] << 16) * inv, __uint_as_float(v[2 * e] & 0xffff0000u) * inv,
-                               __uint_as_float(v[2 * e + 1] << 16) * inv, __uint_as_float(v[2 * e + 1] & 0xffff0000u) * inv, first[e], second[e]);
-                    uint8_t* at = sQ + (lane >> 3) * SLAB + r * 128 + (((lane & 7) ^ (r & 7)) * 16);
-                    *reinterpret_cast<uint4*>(at) = make_uint4(first[0], first[1], first[2], first[3]);
-                    *reinterpret_cast<uint4*>(at + 4 * SLAB) = make_uint4(second[0], second[1], second[2], second[3]);
-                    if (lane == 0) sh->tau[r] = m < 0x7f80u ? __uint_as_float((uint32_t)byte << 23) : __uint_as_float(0x7fc00000u);
-                }
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(cluster_map(&sh->q_full, 0));
-                softmax_sync();
-            }
-            const float tau = E8 ? sh->tau[E8 ? row : 0] : 1.f;
-            uint64_t sees = ~0ull;        // bit i: draft i
-            if (64 * (int)rank + row < n_rows) {
+            const bool mine = 64 * (int)rank + row < n_rows;      // (else nobody's: sees nothing)
+            uint64_t sees = 0;            // bit i: draft i
+            if (mine) {
                 const int j = (tile * 128 + 64 * (int)rank + row) / p.H;
                 sees = p.mask != nullptr ? p.mask[(int64_t)b * p.S + j] : (2ull << j) - 1ull;
             }
+            const float tau = E8 && mine ? p.q_tau[row0 + 64 * (int)rank + row] : 1.f;
             float m_ref = -INFINITY;      // log2 units; 8 bits: of the logits times the tokens' powers of two
-            float m_sum = -INFINITY;      // 8 bits: reference of this thread's row sum
+            float m_sum = -INFINITY;      // 8 bits: reference of this thread's row sum, which is of the logits alone
             float l_part[2] = {0.f, 0.f};
             for (int j = 0; j < n_tiles; ++j) {
                 const int n_valid = j == n_tiles - 1 ? n_last : TOK;
@@ -455,97 +402,85 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                 ok = __all_sync(0xffffffffu, ok);
                 // bit c: token c of this quarter is there, and visible to this row
                 const int t_rel = 32 * quarter, first = tok_begin + j * TOK + t_rel;
-                uint32_t vis = n_valid >= t_rel + 32 ? 0xffffffffu : n_valid > t_rel ? (1u << (n_valid - t_rel)) - 1u : 0u;
+                uint32_t vis = !mine ? 0u : n_valid >= t_rel + 32 ? 0xffffffffu : n_valid > t_rel ? (1u << (n_valid - t_rel)) - 1u : 0u;
                 if (first + 32 > draft0) {
                     const int at = first - draft0;      // > -32
                     vis &= at >= 64 ? 0u : at >= 0 ? (uint32_t)(sees >> at) : ((uint32_t)sees << -at) | ((1u << -at) - 1u);
                 }
-                uint32_t sr[32], pk[16];
-                const float room = m_ref == -INFINITY ? -INFINITY : E8 ? kLog2Off + kLog2Room : kRescale16;     // -inf: any logit exceeds it
-                bool exceed = false;
+                // x[c]: the logit in log2 units, above the reference (8 bits: with the token's power of two, at the offset)
+                float x[32], tsum = 0.f;
+                uint32_t pk[16];
+                float off = (E8 ? kLog2Off : 0.f) - (m_ref == -INFINITY ? 0.f : m_ref), top = -INFINITY;
+                const float4* isc4 = reinterpret_cast<const float4*>(&sh->isc[E8 ? j & 3 : 0][E8 ? t_rel : 0]);
                 const float4* lg4 = reinterpret_cast<const float4*>(&sh->lg[E8 ? j & 3 : 0][E8 ? t_rel : 0]);
+                // P in the form of the product's operand, and (8 bits) its sum without the tokens' powers of two
                 auto probabilities = [&] {
-                    const float off = (E8 ? kLog2Off : 0.f) - (m_ref == -INFINITY ? 0.f : m_ref);
+                    uint64_t sum = 0ull;      // two 32-bit zeros
 #pragma unroll
                     for (int c = 0; c < 32; c += 4) {
-                        const float4 g = E8 ? lg4[c / 4] : make_float4(0.f, 0.f, 0.f, 0.f);
-                        const float a0 = fmaf(__uint_as_float(sr[c]), p.scale_log2, g.x + off), a1 = fmaf(__uint_as_float(sr[c + 1]), p.scale_log2, g.y + off);
-                        const float a2 = fmaf(__uint_as_float(sr[c + 2]), p.scale_log2, g.z + off), a3 = fmaf(__uint_as_float(sr[c + 3]), p.scale_log2, g.w + off);
-                        exceed |= (a0 > room) | (a1 > room) | (a2 > room) | (a3 > room);
-                        const float p0 = fast_exp2(a0), p1 = fast_exp2(a1), p2 = fast_exp2(a2), p3 = fast_exp2(a3);
+                        const float p0 = fast_exp2(x[c]), p1 = fast_exp2(x[c + 1]), p2 = fast_exp2(x[c + 2]), p3 = fast_exp2(x[c + 3]);
                         if (E8) {
-                            split4(p0, p1, p2, p3, pk[c / 4], pk[8 + c / 4]);
+                            const float4 g = isc4[c / 4];
+                            const uint64_t pa = pack_f32x2(p0, p1), pb = pack_f32x2(p2, p3);
+                            sum = fma_f32x2(pa, pack_f32x2(g.x, g.y), sum);
+                            sum = fma_f32x2(pb, pack_f32x2(g.z, g.w), sum);
+                            split4_x2(pa, pb, pk[c / 4], pk[8 + c / 4]);
                         } else {
                             pk[c / 2] = pack_bf16(p0, p1);
                             pk[c / 2 + 1] = pack_bf16(p2, p3);
                         }
                     }
+                    if (E8) {
+                        float a, b2;
+                        unpack_f32x2(sum, a, b2);
+                        tsum = a + b2;
+                    }
                 };
                 if (ok) {
                     tc_fence_after();
                     const uint32_t s_addr = tmem_base + lane_base + 256u + (uint32_t)((j & 1) * (E8 ? 128 : 64) + 32 * w);
+                    uint32_t sr[32];
                     tmem_ld32(s_addr, sr);
+                    const uint64_t off2 = pack_f32x2(off, off), scale2 = pack_f32x2(p.scale_log2, p.scale_log2);
                     if (E8) {
                         uint32_t rr[32];
                         tmem_ld32(s_addr + 64u, rr);
                         tmem_ld_wait();
                         const float4* sc4 = reinterpret_cast<const float4*>(&sh->sc[E8 ? j & 3 : 0][E8 ? t_rel : 0]);
+                        const uint64_t tau2 = pack_f32x2(tau, tau);
 #pragma unroll
                         for (int c = 0; c < 32; c += 4) {
-                            const float4 g = sc4[c / 4];
-                            sr[c] = __float_as_uint(fmaf(__uint_as_float(sr[c]), g.x * tau, __uint_as_float(rr[c])));
-                            sr[c + 1] = __float_as_uint(fmaf(__uint_as_float(sr[c + 1]), g.y * tau, __uint_as_float(rr[c + 1])));
-                            sr[c + 2] = __float_as_uint(fmaf(__uint_as_float(sr[c + 2]), g.z * tau, __uint_as_float(rr[c + 2])));
-                            sr[c + 3] = __float_as_uint(fmaf(__uint_as_float(sr[c + 3]), g.w * tau, __uint_as_float(rr[c + 3])));
+                            const float4 g = sc4[c / 4], e = lg4[c / 4];
+#pragma unroll
+                            for (int i = 0; i < 4; i += 2) {
+                                const uint64_t t1 = mul_f32x2(i == 0 ? pack_f32x2(g.x, g.y) : pack_f32x2(g.z, g.w), tau2);
+                                const uint64_t t2 = add_f32x2(i == 0 ? pack_f32x2(e.x, e.y) : pack_f32x2(e.z, e.w), off2);
+                                const uint64_t r2 = pack_f32x2(__uint_as_float(rr[c + i]), __uint_as_float(rr[c + i + 1]));
+                                const uint64_t s2 = pack_f32x2(__uint_as_float(sr[c + i]), __uint_as_float(sr[c + i + 1]));
+                                unpack_f32x2(fma_f32x2(s2, t1, fma_f32x2(r2, scale2, t2)), x[c + i], x[c + i + 1]);
+                            }
                         }
                     } else {
                         tmem_ld_wait();
+#pragma unroll
+                        for (int c = 0; c < 32; c += 2)
+                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(sr[c]), __uint_as_float(sr[c + 1])), scale2, off2), x[c], x[c + 1]);
                     }
                     if (vis != 0xffffffffu) {
 #pragma unroll
                         for (int c = 0; c < 32; ++c)
-                            if (!((vis >> c) & 1u)) sr[c] = 0xff800000u;
+                            if (!((vis >> c) & 1u)) x[c] = -INFINITY;
                     }
                     // probabilities against the current reference: final unless the CTA votes for a rescale
                     probabilities();
-                    if (E8) {
-                        float mx = -INFINITY;
+                    float mx[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) mx = fmaxf(mx, __uint_as_float(sr[c]));
-                        mx *= p.scale_log2;
-                        if (mx > m_sum + 60.f || m_sum == -INFINITY) {
-                            if (mx != -INFINITY) {
-                                const float f = m_sum == -INFINITY ? 0.f : fast_exp2(m_sum - mx);
-                                l_part[0] *= f;
-                                l_part[1] *= f;
-                                m_sum = mx;
-                            }
-                        }
-                        const float base = m_sum == -INFINITY ? 0.f : m_sum;
-#pragma unroll
-                        for (int c = 0; c < 32; c += 2) {
-                            l_part[0] += fast_exp2(fmaf(__uint_as_float(sr[c]), p.scale_log2, -base));
-                            l_part[1] += fast_exp2(fmaf(__uint_as_float(sr[c + 1]), p.scale_log2, -base));
-                        }
-                    }
+                    for (int c = 4; c < 32; ++c) mx[c & 3] = fmaxf(mx[c & 3], x[c]);
+                    top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                 }
-                if (vote_or(exceed)) {
-                    float mx = -INFINITY;
-                    if (ok) {
-                        if (E8) {
-#pragma unroll
-                            for (int c = 0; c < 32; c += 4) {
-                                const float4 g = lg4[c / 4];
-                                mx = fmaxf(mx, fmaxf(fmaxf(fmaf(__uint_as_float(sr[c]), p.scale_log2, g.x), fmaf(__uint_as_float(sr[c + 1]), p.scale_log2, g.y)),
-                                                     fmaxf(fmaf(__uint_as_float(sr[c + 2]), p.scale_log2, g.z), fmaf(__uint_as_float(sr[c + 3]), p.scale_log2, g.w))));
-                            }
-                        } else {
-#pragma unroll
-                            for (int c = 0; c < 32; ++c) mx = fmaxf(mx, __uint_as_float(sr[c]));
-                            mx *= p.scale_log2;
-                        }
-                    }
-                    sh->red[quarter][row] = mx;
+                // (a row without a reference: any logit exceeds it)
+                if (vote_or(top > (m_ref == -INFINITY ? -INFINITY : E8 ? kLog2Off + kLog2Room : kRescale16))) {
+                    sh->red[quarter][row] = top - off;
                     softmax_sync();
                     const float cm = fmaxf(fmaxf(sh->red[0][row], sh->red[1][row]), fmaxf(sh->red[2][row], sh->red[3][row]));
                     const float m_new = fmaxf(m_ref, cm);
@@ -573,7 +508,44 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                         }
                         tmem_st_wait();
                     }
-                    if (ok) probabilities();
+                    if (ok) {
+                        const float off_new = (E8 ? kLog2Off : 0.f) - (m_ref == -INFINITY ? 0.f : m_ref), d = off_new - off;
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) x[c] += d;
+                        off = off_new;
+                        probabilities();
+                    }
+                }
+                if (E8 && ok) {
+                    // Row sum of 2^(logit - m_sum).  P holds the tokens' powers of two, so its sum without them is 2^off of that: exact as
+                    // long as they are within 2^+-40 (nothing that counts is lost where P underflows); else from the logits themselves.
+                    if (!sh->wide[E8 ? j & 3 : 0]) {
+                        if (m_sum == -INFINITY || -off - m_sum > 40.f) {
+                            l_part[0] = m_sum == -INFINITY ? 0.f : l_part[0] * fast_exp2(m_sum + off);
+                            m_sum = -off;
+                        }
+                        l_part[0] = fmaf(tsum, fast_exp2(-off - m_sum), l_part[0]);
+                    } else {
+                        float mx = -INFINITY;
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            const float4 e = lg4[c];
+                            const float y0 = x[4 * c] - e.x, y1 = x[4 * c + 1] - e.y, y2 = x[4 * c + 2] - e.z, y3 = x[4 * c + 3] - e.w;
+                            mx = fmaxf(mx, fmaxf(fmaxf(y0, y1), fmaxf(y2, y3)));
+                        }
+                        mx -= off;
+                        if (mx != -INFINITY && (m_sum == -INFINITY || mx - m_sum > 40.f)) {
+                            l_part[0] = m_sum == -INFINITY ? 0.f : l_part[0] * fast_exp2(m_sum - mx);
+                            m_sum = mx;
+                        }
+                        const float base = off + (m_sum == -INFINITY ? 0.f : m_sum);
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            const float4 e = lg4[c];
+                            l_part[0] += (fast_exp2(x[4 * c] - e.x - base) + fast_exp2(x[4 * c + 1] - e.y - base)) +
+                                         (fast_exp2(x[4 * c + 2] - e.z - base) + fast_exp2(x[4 * c + 3] - e.w - base));
+                        }
+                    }
                 }
                 if (ok) {
                     if (!E8) {
@@ -722,19 +694,25 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                                            : *reinterpret_cast<const uint32_t*>(p.exponents + (int64_t)page * p.page_size + t0 % p.page_size);
             };
             uint32_t next = load(0);
+            bool wide = false;
             for (int j = 0; j < n_tiles; ++j) {
                 const uint32_t bytes = next;
                 next = load(j + 1);
                 if (j >= 4 && !mbar_wait_warp(&sh->sc_empty[j & 3], ((j >> 2) & 1) ^ 1, abort_flag)) break;
-                float sc[4], lg[4];
+                float sc[4], lg[4], isc[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const uint32_t e = (bytes >> (8 * i)) & 0xffu;
-                    sc[i] = e == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(e << 23);    // (byte 0, 2^-127: zero)
+                    sc[i] = (e == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(e << 23)) * p.scale_log2;    // (byte 0, 2^-127: zero)
                     lg[i] = (float)((int)e - 127);
+                    isc[i] = e == 255u ? 1.f : __uint_as_float((254u - e) << 23);
+                    wide = wide || (e != 255u && (e < 87u || e > 167u) && tok_begin + j * TOK + 4 * lane + i < tok_end);
                 }
+                wide = __any_sync(0xffffffffu, wide);
                 *reinterpret_cast<float4*>(&sh->sc[E8 ? j & 3 : 0][E8 ? 4 * lane : 0]) = make_float4(sc[0], sc[1], sc[2], sc[3]);
                 *reinterpret_cast<float4*>(&sh->lg[E8 ? j & 3 : 0][E8 ? 4 * lane : 0]) = make_float4(lg[0], lg[1], lg[2], lg[3]);
+                *reinterpret_cast<float4*>(&sh->isc[E8 ? j & 3 : 0][E8 ? 4 * lane : 0]) = make_float4(isc[0], isc[1], isc[2], isc[3]);
+                if (lane == 0) sh->wide[E8 ? j & 3 : 0] = wide;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh->sc_full[j & 3]);
             }
@@ -818,7 +796,7 @@ cudaError_t launch_draft_sm100(const DraftAttn& a, void* o_lat_direct, float* ls
     const bool direct = o_lat_direct != nullptr;
     CUtensorMap tm_qa, tm_qp, tm_ckv, tm_kpe, tm_o;
     uint32_t box[2] = {64, 64};
-    {   // the queries as one [B * rows, 512] matrix; rows past the end read as zeros
+    {   // the queries as one matrix of 1 KB rows (512 values, or both terms of 512); rows past the end read as zeros
         uint64_t dims[2] = {512, (uint64_t)all_rows};
         uint64_t str[1] = {512 * 2};
         cudaError_t e = make_tmap_bf16(&tm_qa, a.q_abs, 2, dims, str, box);
@@ -847,7 +825,7 @@ cudaError_t launch_draft_sm100(const DraftAttn& a, void* o_lat_direct, float* ls
     p.scale_log2 = a.scale * kLog2e;
     p.lse_part = a.lse_part;
     p.o_lat_direct = static_cast<__nv_bfloat16*>(o_lat_direct); p.lse_direct = lse_direct; p.status = status;
-    p.q_abs = static_cast<const __nv_bfloat16*>(a.q_abs); p.exponents = a.cache->ckv_exponents;
+    p.q_tau = a.q_tau; p.exponents = a.cache->ckv_exponents;
     const int64_t items = (int64_t)p.row_tiles * a.n_chunks * a.B;
     if (items > INT32_MAX / 2) return cudaErrorInvalidValue;
     p.l2_base = static_cast<const char*>(a.w_uv);

@@ -110,11 +110,14 @@ cudaError_t make_q_absorb_tmap(const void* w_uk_t, int H, CUtensorMap* tm_w);
 // with desc given, one int4 per launch position {request, clamped suffix length, first page, second page}
 // (-1 where the block table has no such column) that saves the absorb kernel three dependent loads.
 // n_requests > 0: that many requests have lengths and table rows, fewer than the B query rows.
+// q_terms and q_tau ([B, H]) given: a row is written as E4M3 codes of two terms [2][512] and the power of two that their sum is to be
+// multiplied by (the smallest under which the row's largest value fits 448); q_abs may then be null.
 // walk_ctas > 0 (and B <= 128): that many CTAs walk through the heads instead of one CTA per head (for launches that share the
 // GPU with a kernel that leaves only a few SMs free).
 cudaError_t launch_q_absorb_sm100(const void* q_nope, const CUtensorMap* tm_w, void* q_abs, int B, int H, int n_sm, int walk_ctas, int* status,
                                   const int32_t* seq_lens, int32_t* order, const int32_t* block_table, int max_pages,
-                                  int page_size, int32_t* desc, cudaStream_t s, int n_requests = 0);
+                                  int page_size, int32_t* desc, cudaStream_t s, int n_requests = 0, void* q_terms = nullptr,
+                                  float* q_tau = nullptr);
 
 // Naive shared-prefix attention partials (Algorithm 1 line 4).
 struct NaiveAttn {
@@ -223,7 +226,8 @@ cudaError_t launch_absorb_pair_sm100(const AbsorbAttn& a, int64_t Ls_pad, void* 
 // Partials go to slots [chunk0, chunk0 + n_chunks) of o_part / lse_part, or, with o_lat_direct (a single chunk in all), the merged
 // bf16 latent output [B * S, H, 512] and its LSE there.
 struct DraftAttn {
-    const void* q_abs; const void* q_pe;           // [B*S,H,512], [B*S,H,64]
+    const void* q_abs; const void* q_pe;           // [B*S,H,512] (8-bit cache: the two terms, see launch_q_absorb_sm100), [B*S,H,64]
+    const float* q_tau;                            // 8-bit cache: [B*S,H]
     const typhoon_mla_cache_t* cache;
     const int32_t* block_table; int max_pages; const int32_t* seq_lens;
     const int32_t* draft_lens;                     // optional [B]: how many of the suffix's last tokens are drafts (else S)

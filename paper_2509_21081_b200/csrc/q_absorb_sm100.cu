@@ -34,6 +34,8 @@ constexpr int SMEM_BYTES_DIRECT = A_BYTES + W_BYTES + 1024 + 256;
 
 struct QAbsorbParams {
     void* q_abs;   // bf16 [B, H, 512]
+    void* q_terms; // E4M3 codes [B, H, 2, 512]
+    float* q_tau;  // ... and their powers of two [B, H]
     int B, H;
     int n_tiles, splits;   // tiles of 128 requests; CTAs per head (CTA s takes tiles s, s + splits, ...)
     int walk_ctas;         // > 0: walk mode with this many working CTAs (1-D grid, block walk_ctas is the ordering block)
@@ -49,9 +51,13 @@ struct QAbsorbParams {
     int4* desc;
 };
 
+// FORM & 1: the result leaves in bf16.  FORM & 2: as two E4M3 terms under a power of two per row, for products with an 8-bit cache
+// (draft_pair_sm100.cu); each thread has its row's 512 values in tensor memory and goes through them twice, for the largest and for the
+// codes.
+template <int FORM>
 __global__ void __launch_bounds__(192, 1)
 q_absorb_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_w,
-                      const __grid_constant__ CUtensorMap tm_out, QAbsorbParams p) {
+                      const __grid_constant__ CUtensorMap tm_out, const __grid_constant__ CUtensorMap tm_terms, QAbsorbParams p) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     pdl_trigger();
@@ -173,6 +179,30 @@ q_absorb_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             tc_fence_after();
             const int b0 = tile_of(k) * 128;
             const int h = head_of(k);
+            float inv = 1.f;
+            if (FORM & 2) {
+                uint32_t m = 0;      // bits of the largest magnitude (not finite: at least 0x7f800000)
+#pragma unroll 1
+                for (int c = 0; c < 16; ++c) {
+                    uint32_t r[32];
+                    tmem_ld32(tmem_base + ((uint32_t)lg << 16) + c * 32, r);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) m = max(m, r[j] & 0x7fffffffu);
+                }
+                // exponent field of the smallest power of two under which it fits 448 = 1.75 * 2^8, where that and its inverse are
+                // normal numbers
+                const int byte = min(max((int)(m >> 23) - 8 + ((m & 0x7fffffu) > 0x600000u ? 1 : 0), 1), 247);
+                inv = __uint_as_float((uint32_t)(254 - byte) << 23);
+                if (b0 + row < p.B) p.q_tau[(int64_t)(b0 + row) * p.H + h] = __uint_as_float(m < 0x7f800000u ? (uint32_t)byte << 23 : 0x7fc00000u);
+            }
+            // 32 values as 8 words of each term
+            auto terms = [&](const uint32_t (&r)[32], uint32_t (&first)[8], uint32_t (&second)[8]) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    split4(__uint_as_float(r[4 * j]) * inv, __uint_as_float(r[4 * j + 1]) * inv, __uint_as_float(r[4 * j + 2]) * inv,
+                           __uint_as_float(r[4 * j + 3]) * inv, first[j], second[j]);
+            };
             if (p.B <= DIRECT_ROWS) {
                 // A handful of requests (one warp's rows at most): the staged store's two block-wide barriers per
                 // result block cost more than they save; every thread writes its own row.
@@ -182,7 +212,18 @@ q_absorb_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                     uint32_t r[32];
                     tmem_ld32(tmem_base + ((uint32_t)lg << 16) + c * 32, r);
                     tmem_ld_wait();
-                    if (b0 + row < p.B) {
+                    if (FORM & 2) {
+                        uint32_t t[2][8];
+                        terms(r, t[0], t[1]);
+                        uint8_t* dst8 = reinterpret_cast<uint8_t*>(p.q_terms) + ((int64_t)(b0 + row) * p.H + h) * 1024;
+                        if (b0 + row < p.B) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                *reinterpret_cast<uint4*>(dst8 + 512 * (j >> 1) + c * 32 + 16 * (j & 1)) =
+                                    make_uint4(t[j >> 1][4 * (j & 1)], t[j >> 1][4 * (j & 1) + 1], t[j >> 1][4 * (j & 1) + 2], t[j >> 1][4 * (j & 1) + 3]);
+                        }
+                    }
+                    if ((FORM & 1) && b0 + row < p.B) {
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             uint4 v;
@@ -198,8 +239,11 @@ q_absorb_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                 mbar_arrive(acc_empty);
                 continue;
             }
+            constexpr int FORMS = FORM == 3 ? 2 : 1;
 #pragma unroll 1
-            for (int n = 0; n < 4; ++n, ++blk) {
+            for (int i = 0; i < 4 * FORMS; ++i, ++blk) {
+                const int n = i / FORMS;
+                const bool as_terms = FORM == 2 || (FORM == 3 && (i & 1));
                 uint8_t* stage = sOut + (blk & 1) * STAGE_BYTES;
                 // the store that read this staging buffer two blocks ago must have finished reading it
                 if (leader) bulk_wait_read_n<1>();
@@ -209,6 +253,15 @@ q_absorb_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                     uint32_t r[32];
                     tmem_ld32(tmem_base + ((uint32_t)lg << 16) + n * 128 + c * 32, r);
                     tmem_ld_wait();
+                    if (as_terms) {      // 32 columns = 32 bytes of this row in either term's slab
+                        uint32_t t[2][8];
+                        terms(r, t[0], t[1]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            *reinterpret_cast<uint4*>(stage + (j >> 1) * 16384 + row * 128 + (((2 * c + (j & 1)) ^ (row & 7)) * 16)) =
+                                make_uint4(t[j >> 1][4 * (j & 1)], t[j >> 1][4 * (j & 1) + 1], t[j >> 1][4 * (j & 1) + 2], t[j >> 1][4 * (j & 1) + 3]);
+                        continue;
+                    }
                     // 32 columns = 64 bytes of this row in slab c / 2: 16-byte chunks (c & 1) * 4 + j, swizzled by row
                     uint8_t* srow = stage + (c >> 1) * 16384 + row * 128;
 #pragma unroll
@@ -222,15 +275,16 @@ q_absorb_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                         *reinterpret_cast<uint4*>(srow + ch * 16) = v;
                     }
                 }
-                if (n == 3) {   // all four blocks of this tile have left tensor memory
+                if (i == 4 * FORMS - 1) {   // all four blocks of this tile have left tensor memory
                     tc_fence_before();
                     mbar_arrive(acc_empty);
                 }
                 fence_proxy_async();
                 asm volatile("bar.sync 1, 128;\n" ::: "memory");
                 if (leader) {
-                    tma_store_3d(&tm_out, stage, n * 128, h, b0);
-                    tma_store_3d(&tm_out, stage + 16384, n * 128 + 64, h, b0);
+                    const CUtensorMap* to = as_terms ? &tm_terms : &tm_out;
+                    tma_store_3d(to, stage, as_terms ? n * 64 : n * 128, h, b0);
+                    tma_store_3d(to, stage + 16384, as_terms ? 256 + n * 64 : n * 128 + 64, h, b0);
                     bulk_commit();
                 }
             }
@@ -255,7 +309,10 @@ q_absorb_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
 }  // namespace
 
 cudaError_t set_attrs_q_absorb_sm100() {
-    return cudaFuncSetAttribute(q_absorb_sm100_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+    cudaError_t e = cudaSuccess;
+    for (auto* kernel : {q_absorb_sm100_kernel<1>, q_absorb_sm100_kernel<2>, q_absorb_sm100_kernel<3>})
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+    return e;
 }
 
 cudaError_t make_q_absorb_tmap(const void* w_uk_t, int H, CUtensorMap* tm_w) {
@@ -267,10 +324,10 @@ cudaError_t make_q_absorb_tmap(const void* w_uk_t, int H, CUtensorMap* tm_w) {
 
 cudaError_t launch_q_absorb_sm100(const void* q_nope, const CUtensorMap* tm_w, void* q_abs, int B, int H, int n_sm, int walk_ctas, int* status,
                                   const int32_t* seq_lens, int32_t* order, const int32_t* block_table, int max_pages,
-                                  int page_size, int32_t* desc, cudaStream_t s, int n_requests) {
+                                  int page_size, int32_t* desc, cudaStream_t s, int n_requests, void* q_terms, float* q_tau) {
     if (B <= 0) return cudaSuccess;
     if (n_requests <= 0) n_requests = B;
-    CUtensorMap tm_q, tm_out;
+    CUtensorMap tm_q, tm_out, tm_terms;
     {
         uint64_t dims[3] = {128, (uint64_t)H, (uint64_t)B};
         uint64_t str[2] = {128 * 2, (uint64_t)H * 128 * 2};
@@ -282,7 +339,10 @@ cudaError_t launch_q_absorb_sm100(const void* q_nope, const CUtensorMap* tm_w, v
         uint64_t dims[3] = {512, (uint64_t)H, (uint64_t)B};
         uint64_t str[2] = {512 * 2, (uint64_t)H * 512 * 2};
         uint32_t box[3] = {64, 1, 128};
-        cudaError_t e = make_tmap_bf16(&tm_out, q_abs, 3, dims, str, box);
+        cudaError_t e = make_tmap_bf16(&tm_out, q_abs ? q_abs : q_terms, 3, dims, str, box);   // (both have rows of 1 KB)
+        if (e != cudaSuccess) return e;
+        tm_terms = tm_out;
+        if (q_terms && q_abs) e = make_tmap_bf16(&tm_terms, q_terms, 3, dims, str, box);
         if (e != cudaSuccess) return e;
     }
     const bool with_order = seq_lens != nullptr && order != nullptr && n_requests <= 4096;
@@ -292,10 +352,11 @@ cudaError_t launch_q_absorb_sm100(const void* q_nope, const CUtensorMap* tm_w, v
     const int splits = std::max(1, std::min(n_tiles, std::max(n_sm, 1) / H));
     // walk mode only with one request tile per head and fewer working CTAs than heads
     const int walk = (n_tiles == 1 && walk_ctas > 0 && walk_ctas < H) ? walk_ctas : 0;
-    QAbsorbParams p{q_abs, B, H, n_tiles, splits, walk, status, seq_lens, order, n_requests, block_table, max_pages, page_size,
+    QAbsorbParams p{q_abs, q_terms, q_tau, B, H, n_tiles, splits, walk, status, seq_lens, order, n_requests, block_table, max_pages, page_size,
                     (with_order && block_table != nullptr) ? reinterpret_cast<int4*>(desc) : nullptr};
     const dim3 grid = walk ? dim3(walk + (with_order ? 1 : 0), 1, 1) : dim3(splits, H + (with_order ? 1 : 0), 1);
-    return launch_pdl(q_absorb_sm100_kernel, grid, dim3(192), B <= DIRECT_ROWS ? SMEM_BYTES_DIRECT : SMEM_BYTES, s, tm_q, *tm_w, tm_out, p);
+    auto* kernel = !q_terms ? q_absorb_sm100_kernel<1> : q_abs ? q_absorb_sm100_kernel<3> : q_absorb_sm100_kernel<2>;
+    return launch_pdl(kernel, grid, dim3(192), B <= DIRECT_ROWS ? SMEM_BYTES_DIRECT : SMEM_BYTES, s, tm_q, *tm_w, tm_out, tm_terms, p);
 }
 
 }  // namespace tmla

@@ -423,6 +423,26 @@ __device__ __forceinline__ void tma_store_4d(const CUtensorMap* m, const void* s
                  : "memory");
 }
 
+// ---------------------------------------------------------------- E4M3
+// Two E4M3 codes (low byte: a) and what is left of the pair.
+__device__ __forceinline__ uint32_t e4m3_pair(float a, float b) {
+    uint16_t d;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(d) : "f"(b), "f"(a));
+    return d;
+}
+__device__ __forceinline__ float2 e4m3_values(uint32_t codes) {
+    uint32_t h2;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(h2) : "h"((uint16_t)codes));
+    return __half22float2(*reinterpret_cast<__half2*>(&h2));
+}
+// Four values as codes of two terms: the nearest E4M3 number, and the nearest one to the rest.
+__device__ __forceinline__ void split4(float a, float b, float c, float d, uint32_t& first, uint32_t& second) {
+    const uint32_t x = e4m3_pair(a, b), y = e4m3_pair(c, d);
+    const float2 u = e4m3_values(x), v = e4m3_values(y);
+    first = x | (y << 16);
+    second = e4m3_pair(a - u.x, b - u.y) | (e4m3_pair(c - v.x, d - v.y) << 16);
+}
+
 // ---------------------------------------------------------------- packed fp32 arithmetic
 // Two fp32 lanes per instruction (sm_100): the softmax loops do their scale-and-subtract and their row sums
 // on pairs, which halves the issue slots those take next to the exponentials.
@@ -472,6 +492,23 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;\n" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
+}
+
+// split4 of two packed pairs of non-negative values.  The first term is the value rounded to 4 significant bits by Dekker's splitting (with
+// 2^20 + 1), which is the nearest E4M3 number where that is a normal one and within half a step of the smallest below; the codes then
+// convert without a way back from the first.
+__device__ __forceinline__ void split4_x2(uint64_t ab, uint64_t cd, uint32_t& first, uint32_t& second) {
+    const uint64_t k = pack_f32x2(1048577.f, 1048577.f), minus = pack_f32x2(-1.f, -1.f);
+    const uint64_t u = mul_f32x2(ab, k), v = mul_f32x2(cd, k);
+    const uint64_t hu = fma_f32x2(fma_f32x2(ab, minus, u), minus, u), hv = fma_f32x2(fma_f32x2(cd, minus, v), minus, v);
+    const uint64_t lu = fma_f32x2(hu, minus, ab), lv = fma_f32x2(hv, minus, cd);
+    float a, b, c, d;
+    unpack_f32x2(hu, a, b);
+    unpack_f32x2(hv, c, d);
+    first = e4m3_pair(a, b) | (e4m3_pair(c, d) << 16);
+    unpack_f32x2(lu, a, b);
+    unpack_f32x2(lv, c, d);
+    second = e4m3_pair(a, b) | (e4m3_pair(c, d) << 16);
 }
 
 // ---------------------------------------------------------------- TMEM <-> registers
