@@ -1104,7 +1104,7 @@ static int decode_core(const Settings& cfg, const typhoon_mla_shared* sh, const 
         if (draft && e == cudaSuccess) {
             if (pl.n_shared_chunks > 0) ++launches;
             const DraftAttn da{q_terms ? q_terms : q_abs, q_pe, q_tau, draft->cache, block_table, max_pages, seq_lens, draft->draft_lens, draft->mask, desc, draft->n_requests,
-                               draft->S, H, pl.draft_chunk, pl.n_suffix_chunks, pl.n_shared_chunks, softmax_scale, o_part_a, lse_part_a,
+                               draft->S, H, pl.draft_chunk, pl.n_suffix_chunks, pl.n_shared_chunks, sh->num_sms, softmax_scale, o_part_a, lse_part_a,
                                forked ? nullptr : sh->w_uv};
             e = launch_draft_sm100(da, n_chunks == 1 ? o_lat : nullptr, lse_a, sh->status, s);
         }

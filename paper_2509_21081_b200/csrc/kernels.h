@@ -234,6 +234,7 @@ struct DraftAttn {
     const uint64_t* mask;                          // optional [B,S]: bit i, draft i is visible to the row (else 0 .. j to row j)
     const int32_t* desc;                           // optional [B][4]: per launch position, see launch_q_absorb_sm100
     int B, S, H; int chunk, n_chunks, chunk0;
+    int n_sm;
     float scale;
     float* o_part;   // [slots][B*S][H][512], each normalised
     float* lse_part; // [slots][B*S][H]
