@@ -58,6 +58,7 @@ struct DraftParams {
     const uint64_t* mask;        // optional [B, S]
     const int4* desc;      // optional, per launch position: {request, clamped suffix length, page 0, page 1}
     float scale_log2;
+    float* o_part;         // [slots][B * rows][512]
     float* lse_part;       // [slots][B * rows]
     __nv_bfloat16* o_lat_direct;   // single chunk: the merged result bf16 [B * rows][512], and its LSE
     float* lse_direct;
@@ -96,7 +97,6 @@ struct Shared {
     uint64_t o_done[2];               // second product of tile j: o_done[j & 1]
     uint64_t v_tail[2];               // own copies of the second operand of a tile whose values are gone through first (8 bits: per stage)
     uint64_t q_empty;                 // the last logits of an item are there (both CTAs)
-    uint64_t v_free;                  // the second operand's space has served the item's epilogue: one arrival per part of a tile
     uint64_t sc_full[4], sc_empty[4]; // 8 bits: powers of two of tile j in slot j & 3; one arrival per softmax warp when they are read
     uint32_t tmem_base;
     int abort_flag;
@@ -128,6 +128,12 @@ __device__ __forceinline__ bool vote_or(bool pred) {   // over the N softmax thr
 template <int N>
 __device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync %0, %1;\n" ::"n"(kSoftmaxBar), "n"(N) : "memory"); }
 
+// 32 bytes of one row
+__device__ __forceinline__ void store_sector(void* p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
+                 "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
 template <int N>
 __device__ __forceinline__ float max_of(const float (&x)[N]) {
     static_assert(N % 4 == 0 || N == 1, "");
@@ -144,8 +150,7 @@ __device__ __forceinline__ float max_of(const float (&x)[N]) {
 template <bool E8>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<E8>::THREADS, 1)
 draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constant__ CUtensorMap tm_qp,
-                        const __grid_constant__ CUtensorMap tm_ckv, const __grid_constant__ CUtensorMap tm_kpe,
-                        const __grid_constant__ CUtensorMap tm_o, DraftParams p) {
+                        const __grid_constant__ CUtensorMap tm_ckv, const __grid_constant__ CUtensorMap tm_kpe, DraftParams p) {
     using X = Shape<E8>;
     constexpr int KS = X::KS, VS = X::VS, LAT = X::LAT, HALF = LAT / 2, TPT = X::TPT, PARTS = X::PARTS, SM = 32 * X::WARPS;
     extern __shared__ uint8_t smem_raw[];
@@ -165,7 +170,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
         uint64_t* all = &sh->q_full;
         constexpr int n_bars = (int)(offsetof(Shared<E8>, tmem_base) / sizeof(uint64_t));
         static_assert(n_bars <= 32, "one lane per barrier");
-        if (lane < n_bars) mbar_init(all + lane, all + lane == &sh->p_ready ? 2 * X::WARPS : all + lane == &sh->v_free ? PARTS : all + lane >= &sh->sc_empty[0] ? X::WARPS : 1);
+        if (lane < n_bars) mbar_init(all + lane, all + lane == &sh->p_ready ? 2 * X::WARPS : all + lane >= &sh->sc_empty[0] ? X::WARPS : 1);
         if (lane == 0) sh->abort_flag = 0;
         fence_mbar_init();
         __syncwarp();
@@ -195,31 +200,30 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
         int draft0;               // first draft
         int first_special;        // tiles from this one on are gone through in shared memory before the second product
     };
-    auto item_at = [&](int k) {
-        Item it;
-        const int i = k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair);
-        it.tile = i % p.row_tiles;
-        it.chunk = (i / p.row_tiles) % p.n_chunks;
-        const int z = i / (p.row_tiles * p.n_chunks);
-        it.pg0 = it.pg1 = -1;
-        int len = 0;
-        it.b = 0;
-        if (i < n_items && k >= 0) {
-            if (p.desc != nullptr) {
-                const int4 d = p.desc[z];
-                it.b = d.x; len = d.y; it.pg0 = d.z; it.pg1 = d.w;
-            } else {
-                it.b = z;
-                len = min(max(p.seq_lens[z], 0), p.max_pages * p.page_size);
-            }
-        } else {
-            it.tile = -1;         // no item
+    auto item_index = [&](int k) { return k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair); };
+    // {request, clamped suffix length, first two pages} of item k; length -1: no such item
+    auto desc_of = [&](int k) {
+        const int i = item_index(k);
+        int4 d = make_int4(0, -1, -1, -1);
+        if (i < n_items) {
+            const int z = i / (p.row_tiles * p.n_chunks);
+            if (p.desc != nullptr) d = p.desc[z];
+            else d = make_int4(z, min(max(p.seq_lens[z], 0), p.max_pages * p.page_size), -1, -1);
         }
+        return d;
+    };
+    auto item_at = [&](int k, int4 d) {
+        Item it;
+        const int i = item_index(k);
         // (through shuffles: the role warps' loops are then known to be uniform)
-        len = __shfl_sync(0xffffffffu, len, 0);
-        it.b = __shfl_sync(0xffffffffu, it.b, 0);
+        const int len = __shfl_sync(0xffffffffu, d.y, 0);
+        it.b = __shfl_sync(0xffffffffu, d.x, 0);
+        it.pg0 = d.z;
+        it.pg1 = d.w;
+        it.tile = len < 0 ? -1 : i % p.row_tiles;
+        it.chunk = (i / p.row_tiles) % p.n_chunks;
         it.tok_begin = it.chunk * p.chunk;
-        it.tok_end = min(len, it.tok_begin + p.chunk);
+        it.tok_end = min(max(len, 0), it.tok_begin + p.chunk);
         it.n_tiles = it.tok_end > it.tok_begin ? (it.tok_end - it.tok_begin + TOK - 1) / TOK : 0;
         it.n_last = it.tok_end - it.tok_begin - (it.n_tiles - 1) * TOK;
         // (a single token that sees itself hides nothing: no draft)
@@ -259,13 +263,13 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
         const uint32_t ld = elect_one() ? 1u : 0u;
         const uint32_t ld_even = rank == 0 ? ld : 0u;
         // tiles are requested into L2 KS + 1 ahead of the load into a freed stage, the next item's as well
-        Item pf = item_at(0);
+        Item pf = item_at(0, desc_of(0));
         int pf_k = 0, pf_j = 0;
         auto prefetch_next = [&] {
             while (pf_k < n_rounds && pf_j >= pf.n_tiles) {
                 ++pf_k;
                 pf_j = 0;
-                if (pf_k < n_rounds) pf = item_at(pf_k);
+                if (pf_k < n_rounds) pf = item_at(pf_k, desc_of(pf_k));
             }
             if (pf_k >= n_rounds) return;
             int page, slot;
@@ -278,7 +282,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
         bool ok = true;
         int g = 0, n = 0;
         for (int k = 0; k < n_rounds && ok; ++k) {
-            const Item it = item_at(k);
+            const Item it = item_at(k, desc_of(k));
             for (int j = 0; j < it.n_tiles && ok; ++j, ++g) {
                 int page, slot;
                 page_of(it, j, (int)rank, page, slot);
@@ -320,26 +324,23 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
         const uint32_t vf[2] = {cluster_map(&sh->v_full[0], 0), cluster_map(&sh->v_full[1], 0)};
         const uint32_t vt[2] = {cluster_map(&sh->v_tail[0], rank), cluster_map(&sh->v_tail[1], rank)};
         bool ok = true;
-        int g = 0, n = 0;
+        int g = 0;
         for (int k = 0; k < n_rounds && ok; ++k) {
-            const Item it = item_at(k);
+            const Item it = item_at(k, desc_of(k));
             for (int j = 0; j < it.n_tiles && ok; ++j, ++g) {
                 int page[2], slot[2];
                 page_of(it, j, 0, page[0], slot[0]);
                 page_of(it, j, 1, page[1], slot[1]);
                 const bool special = j >= it.first_special;  // counted by the CTA's own barrier: its threads go through the values
-                if (j == 0 && n > 0) ok = mbar_wait_warp(&sh->v_free, (n - 1) & 1, abort_flag);
                 const int st = g % VS;
                 uint8_t* dst = sV + st * X::V_BYTES;
-                if (ok && special && g >= VS)     // (the barrier's phases follow one another)
-                    ok = mbar_wait_warp(&sh->v_empty[E8 ? st : 1], ((g / VS) & 1) ^ 1, abort_flag);
-                if (!ok) break;
-                if (special) mbar_arrive_expect_tx_if(ld, &sh->v_tail[st], X::V_BYTES);
 #pragma unroll
                 for (int nb = 0; nb < X::NV; ++nb) {
                     const int i = E8 ? st : nb;
                     if (g >= VS) ok = ok && mbar_wait_warp(&sh->v_empty[i], ((g / VS) & 1) ^ 1, abort_flag);
                     if (!ok) break;
+                    // (v_empty of the first block: the softmax of the stage's previous tile is past its wait on v_tail)
+                    if (special && nb == 0) mbar_arrive_expect_tx_if(ld, &sh->v_tail[st], X::V_BYTES);
                     if (!special) mbar_arrive_expect_tx_if(ld_even, &sh->v_full[i], 2 * X::V_BYTES / X::NV);
                     const uint32_t bar = special ? (st ? vt[1] : vt[0]) : (i ? vf[1] : vf[0]);
                     // 16 bits: blocks of 128 dims, [block][token half][2 slabs]; 8 bits: [token half][2 slabs = blocks]
@@ -350,7 +351,6 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                 if (special) ++issued_t[st];
                 else ++issued_v[st];
             }
-            if (it.n_tiles > 0) ++n;
         }
     } else if (warp == 1 && rank == 0) {
         // ---------------- both products (even CTA)
@@ -362,7 +362,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
         int g = 0, n = 0;
         uint32_t v_phase = 0;               // bit i: parity of the next phase of v_full[i] (per stage; only plain tiles have one)
         for (int k = 0; k < n_rounds && ok; ++k) {
-            const Item it = item_at(k);
+            const Item it = item_at(k, desc_of(k));
             if (it.n_tiles == 0) continue;
             ok = mbar_wait_warp(&sh->q_full, n & 1, abort_flag);
             ++n;
@@ -479,8 +479,10 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
         const bool direct = p.o_lat_direct != nullptr;
         int g = 0;
         uint32_t t_phase = 0;               // bit i: parity of the next phase of v_tail[i]
+        int4 next = desc_of(0);
         for (int k = 0; k < n_rounds; ++k) {
-            const Item it = item_at(k);
+            const Item it = item_at(k, next);
+            next = desc_of(k + 1);        // (asked for an item ahead)
             if (it.tile < 0) continue;
             const int n_rows = min(128, p.rows - it.tile * 128);
             const int64_t row0 = (int64_t)it.b * p.rows + it.tile * 128;
@@ -740,7 +742,6 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
             }
 
             // ---------------- epilogue: row sums, normalised partial, LSE
-            if (vote_or<SM>(*abort_flag != 0)) break;
             sh->red[part][row] = l_part[0] + l_part[1];
             if (E8) sh->red2[E8 ? part : 0][E8 ? row : 0] = m_sum;
             softmax_sync<SM>();
@@ -768,63 +769,41 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                 if (direct) p.lse_direct[r] = lse;
                 else p.lse_part[(p.chunk0 + it.chunk) * all_rows + r] = lse;
             }
-            if (vote_or<SM>(!mbar_wait(&sh->o_done[(g - 1) & 1], ((g - 1) >> 1) & 1, abort_flag))) break;
+            if (vote_or<SM>(*abort_flag != 0 || !mbar_wait(&sh->o_done[(g - 1) & 1], ((g - 1) >> 1) & 1, abort_flag))) break;
             tc_fence_after();
-            // The normalised rows leave through the second operand's space (its last product is done, the next item's first load waits
-            // for v_free) as 128-byte swizzled boxes of 64 rows, in tiled stores that cut off rows past the request's end.  A part's
-            // two warps have one or two boxes there, and this thread's columns are latent dims 256 half + COLS w + 0 .. COLS - 1.
-            constexpr int BOXES = VS * X::V_BYTES / SLAB / PARTS, COLS = 4 * TPT;
-            const int n_box = direct ? COLS / 64 : COLS / 32;  // of a part: 64 bf16 columns, or 32 fp32
-            const bool leader = lane == 0 && (q & 1) == 0;
-            const int box0 = part * n_box;                     // first box of the part, over the 512 dims
+            // The normalised rows go straight from tensor memory to the workspace, a thread its row's 32-byte sectors: through shared memory
+            // and tiled stores the next item's second operand would wait for the space (3500 clocks per item against 1000).  This
+            // thread's columns are latent dims 256 half + 128 w + 0 .. 127.
+            const int64_t r = row0 + 64 * (int)rank + row;
+            const int col0 = 128 * part;
 #pragma unroll 1
-            for (int i = 0; i < n_box; ++i) {
-                uint8_t* box = sV + (part * BOXES + i % BOXES) * SLAB;
-                if (i >= BOXES) {
-                    if (leader) bulk_wait_read_n<BOXES - 1>();
-                    asm volatile("bar.sync %0, 64;\n" ::"r"(2 + part) : "memory");
-                }
-                uint8_t* at = box + row * 128;
+            for (int i = 0; i < 4; ++i) {
+                uint32_t orr[32];
+                tmem_ld32(tmem_base + lane_base + (uint32_t)(128 * w + 32 * i), orr);
+                tmem_ld_wait();
+                if (!mine) continue;
                 if (direct) {
+                    __nv_bfloat16* dst = p.o_lat_direct + r * 512 + col0 + 32 * i;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        uint32_t orr[32];
-                        tmem_ld32(tmem_base + lane_base + (uint32_t)(COLS * w + 64 * i + 32 * e), orr);
-                        tmem_ld_wait();
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t v[8];
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            uint4 v;
-                            uint32_t* vv = reinterpret_cast<uint32_t*>(&v);
-#pragma unroll
-                            for (int f = 0; f < 4; ++f)
-                                vv[f] = pack_bf16(__uint_as_float(orr[8 * c + 2 * f]) * inv, __uint_as_float(orr[8 * c + 2 * f + 1]) * inv);
-                            *reinterpret_cast<uint4*>(at + (((4 * e + c) ^ (row & 7)) * 16)) = v;
-                        }
+                        for (int f = 0; f < 8; ++f)
+                            v[f] = pack_bf16(__uint_as_float(orr[16 * c + 2 * f]) * inv, __uint_as_float(orr[16 * c + 2 * f + 1]) * inv);
+                        store_sector(dst + 16 * c, v);
                     }
                 } else {
-                    uint32_t orr[32];
-                    tmem_ld32(tmem_base + lane_base + (uint32_t)(COLS * w + 32 * i), orr);
-                    tmem_ld_wait();
+                    float* dst = p.o_part + ((int64_t)(p.chunk0 + it.chunk) * all_rows + r) * 512 + col0 + 32 * i;
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        const float4 v = make_float4(__uint_as_float(orr[4 * c]) * inv, __uint_as_float(orr[4 * c + 1]) * inv,
-                                                     __uint_as_float(orr[4 * c + 2]) * inv, __uint_as_float(orr[4 * c + 3]) * inv);
-                        *reinterpret_cast<float4*>(at + ((c ^ (row & 7)) * 16)) = v;
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t v[8];
+#pragma unroll
+                        for (int f = 0; f < 8; ++f) v[f] = __float_as_uint(__uint_as_float(orr[8 * c + f]) * inv);
+                        store_sector(dst + 8 * c, v);
                     }
-                }
-                fence_proxy_async();
-                asm volatile("bar.sync %0, 64;\n" ::"r"(2 + part) : "memory");
-                if (leader) {
-                    if (64 * (int)rank < n_rows)
-                        tma_store_4d(&tm_o, box, (box0 + i) * 64, it.tile * 128 + 64 * (int)rank, it.b, direct ? 0 : p.chunk0 + it.chunk);
-                    bulk_commit();
                 }
             }
             tc_fence_before();
-            if (leader) {
-                bulk_wait_read_n<0>();      // the space must outlive the copies; the kernel end publishes the writes
-                mbar_arrive(&sh->v_free);
-            }
         }
     } else if (E8 && warp == 3) {
         // ---------------- powers of two of a tile's tokens, 4 per lane
@@ -838,7 +817,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
         int g = 0;
         bool ok = true;
         for (int k = 0; k < n_rounds && ok; ++k) {
-            const Item it = item_at(k);
+            const Item it = item_at(k, desc_of(k));
             uint32_t next = load(it, 0);
             for (int j = 0; j < it.n_tiles; ++j, ++g) {
                 const uint32_t bytes = next;
@@ -921,8 +900,7 @@ cudaError_t launch_draft_sm100(const DraftAttn& a, void* o_lat_direct, float* ls
     const bool e8 = a.cache->ckv_exponents != nullptr;
     const int rows = a.S * a.H;
     const int64_t all_rows = (int64_t)a.B * rows;
-    const bool direct = o_lat_direct != nullptr;
-    CUtensorMap tm_qa, tm_qp, tm_ckv, tm_kpe, tm_o;
+    CUtensorMap tm_qa, tm_qp, tm_ckv, tm_kpe;
     uint32_t box[2] = {64, 64};
     {   // the queries as one matrix of 1 KB rows (512 values, or both terms of 512); rows past the end read as zeros
         uint64_t dims[2] = {512, (uint64_t)all_rows};
@@ -936,14 +914,6 @@ cudaError_t launch_draft_sm100(const DraftAttn& a, void* o_lat_direct, float* ls
     }
     cudaError_t e = make_kv_tmaps(*a.cache, &tm_ckv, &tm_kpe);
     if (e != cudaSuccess) return e;
-    {   // output rows as [512 values | rows of a request | requests | slots]; fp32 values are described as pairs of 16-bit elements
-        const uint64_t w = direct ? 512 : 1024;
-        uint64_t dims[4] = {w, (uint64_t)rows, (uint64_t)a.B, direct ? 1u : (uint64_t)(a.chunk0 + a.n_chunks)};
-        uint64_t str[3] = {w * 2, (uint64_t)rows * w * 2, (uint64_t)all_rows * w * 2};
-        uint32_t obox[4] = {64, 64, 1, 1};
-        e = make_tmap_bf16(&tm_o, direct ? o_lat_direct : a.o_part, 4, dims, str, obox);
-        if (e != cudaSuccess) return e;
-    }
     DraftParams p{};
     p.B = a.B; p.S = a.S; p.H = a.H; p.rows = rows;
     p.row_tiles = (rows + 127) / 128; p.chunk = a.chunk; p.n_chunks = a.n_chunks; p.chunk0 = a.chunk0;
@@ -951,7 +921,7 @@ cudaError_t launch_draft_sm100(const DraftAttn& a, void* o_lat_direct, float* ls
     p.block_table = a.block_table; p.seq_lens = a.seq_lens; p.draft_lens = a.draft_lens; p.mask = a.mask;
     p.desc = reinterpret_cast<const int4*>(a.desc);
     p.scale_log2 = a.scale * kLog2e;
-    p.lse_part = a.lse_part;
+    p.o_part = a.o_part; p.lse_part = a.lse_part;
     p.o_lat_direct = static_cast<__nv_bfloat16*>(o_lat_direct); p.lse_direct = lse_direct; p.status = status;
     p.q_tau = a.q_tau; p.exponents = a.cache->ckv_exponents;
     const int64_t items = (int64_t)p.row_tiles * a.n_chunks * a.B;
@@ -961,7 +931,7 @@ cudaError_t launch_draft_sm100(const DraftAttn& a, void* o_lat_direct, float* ls
     const int pairs = (int)std::min<int64_t>(items, std::max(a.n_sm / 2, 1));
     p.l2_bytes = (p.l2_total / (pairs * 32u) / 16u + 1u) * 16u;
     auto* kernel = e8 ? draft_pair_sm100_kernel<true> : draft_pair_sm100_kernel<false>;
-    return launch_pdl(kernel, dim3((unsigned)(2 * pairs)), dim3(e8 ? Shape<true>::THREADS : Shape<false>::THREADS), kDraftSmem, s, tm_qa, tm_qp, tm_ckv, tm_kpe, tm_o, p);
+    return launch_pdl(kernel, dim3((unsigned)(2 * pairs)), dim3(e8 ? Shape<true>::THREADS : Shape<false>::THREADS), kDraftSmem, s, tm_qa, tm_qp, tm_ckv, tm_kpe, p);
 }
 
 }  // namespace tmla
