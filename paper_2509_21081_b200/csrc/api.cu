@@ -359,7 +359,8 @@ Plan draft_floor(const typhoon_mla_shared* sh, int B, int S, int max_pages, int 
     lay_out(&p, B * S, H, floor_chunk_rows(n_sm, rows, absorb_prefix ? sh->Ls : 0, cap), absorb_prefix ? 0 : floor_slot_rows(n_sm, rows, sh->Ls));
     return p;
 }
-Plan make_draft_plan(const typhoon_mla_shared* sh, int schedule, bool stacked, int B, int S, int max_pages, int page_size, int mode) {
+Plan make_draft_plan(const typhoon_mla_shared* sh, int schedule, bool stacked, bool cache_8bit, int B, int S, int max_pages, int page_size,
+                     int mode) {
     const int H = sh->dims.num_heads, n_sm = sh->num_sms > 0 ? sh->num_sms : kDefaultNumSM, Q = B * S;
     const int64_t rows = (int64_t)Q * H, cap = (int64_t)max_pages * page_size;
     const int64_t Ls_absorb = mode == TYPHOON_MLA_MODE_ABSORB ? sh->Ls : 0;
@@ -375,24 +376,32 @@ Plan make_draft_plan(const typhoon_mla_shared* sh, int schedule, bool stacked, i
                          max_slots);
     }
     int max_chunks = (int)std::min<int64_t>(floor_chunk_rows(n_sm, rows, Ls_absorb, cap) / rows, kMaxAbsorbChunks);
-    if (Ls_absorb > 0) {
+    if (Ls_absorb > 0 && cache_8bit) {   // the prefix by the 16-bit kernels
         int none = 0;
         absorb_chunks(true, stacked, false, n_sm, Q, H, Ls_absorb, 0, max_chunks - 1, &p.absorb_pairs, &p.chunk, &p.n_shared_chunks, &none);
         max_chunks -= p.n_shared_chunks;
     }
-    // the suffix: waves x (tiles per chunk + fixed cost in tiles), with the pair kernel's constants (absorb_chunks)
+    // Chunk length of the kernel of drafted tokens (one for prefix and suffixes where it takes both): waves x (tiles per chunk + fixed cost
+    // in tiles), with the pair kernel's constants (absorb_chunks)
+    const int64_t Ls_here = cache_8bit ? 0 : Ls_absorb, longest = std::max(Ls_here, cap);
     double best = 1e30;
     int64_t weighed = 0;
     for (int parts = 1; parts <= max_chunks; ++parts) {
-        const int64_t ch = round_up((cap + parts - 1) / parts, 128);
+        const int64_t ch = round_up((longest + parts - 1) / parts, 128);
         if (ch == weighed) continue;
         weighed = ch;
-        const int64_t n = (cap + ch - 1) / ch, waves = (n * B * row_tiles + n_sm / 2 - 1) / (n_sm / 2);
-        const double cost = (double)waves * ((double)ch / 128 + 4.0 + (n + p.n_shared_chunks > 1 ? 3.0 : 0.0));
+        const int64_t n_sh = (Ls_here + ch - 1) / ch, n_sf = (cap + ch - 1) / ch;
+        if (n_sh + n_sf > max_chunks) break;
+        const int64_t items = n_sh * ((rows + 127) / 128) + n_sf * B * row_tiles, waves = (items + n_sm / 2 - 1) / (n_sm / 2);
+        const double cost = (double)waves * ((double)ch / 128 + 4.0 + (n_sf + n_sh + (cache_8bit ? p.n_shared_chunks : 0) > 1 ? 3.0 : 0.0));
         if (cost < best - 1e-9) {
             best = cost;
             p.draft_chunk = (int)ch;
-            p.n_suffix_chunks = (int)n;
+            p.n_suffix_chunks = (int)n_sf;
+            if (!cache_8bit) {
+                p.chunk = (int)ch;
+                p.n_shared_chunks = (int)n_sh;
+            }
         }
         if (ch <= 128) break;
     }
@@ -1097,14 +1106,17 @@ static int decode_core(const Settings& cfg, const typhoon_mla_shared* sh, const 
                       seq_lens, order, desc, B, H, pl.chunk, pl.n_shared_chunks, draft ? 0 : pl.n_suffix_chunks, softmax_scale,
                       o_part_a, lse_part_a, sh->status, forked ? nullptr : sh->w_uv, draft != nullptr, cfg.stacked_absorb};
         prof_before(TYPHOON_MLA_KERNEL_ABSORB_ATTN, s);
-        if (draft && pl.n_shared_chunks == 0) e = cudaSuccess;   // (the suffix is the kernel's below)
+        // (the kernel of drafted tokens takes the suffixes, and over a 16-bit cache the prefix of an absorb-only step as well)
+        const bool prefix_too = draft && !draft->cache->ckv_exponents;
+        if (draft && (pl.n_shared_chunks == 0 || prefix_too)) e = cudaSuccess;
         else if (!tc) e = launch_absorb_attn_mma(ab, s);
         else if (pl.absorb_pairs) e = launch_absorb_pair_sm100(ab, sh->Ls_pad, o_lat, lse_a, sh->status, s);
         else e = launch_absorb_attn_sm100(ab, &sh->tm_ckv, &sh->tm_kpe_tok, o_lat, lse_a, sh->status, s);
         if (draft && e == cudaSuccess) {
-            if (pl.n_shared_chunks > 0) ++launches;
+            if (pl.n_shared_chunks > 0 && !prefix_too) ++launches;
             const DraftAttn da{q_terms ? q_terms : q_abs, q_pe, q_tau, draft->cache, block_table, max_pages, seq_lens, draft->draft_lens, draft->mask, desc, draft->n_requests,
-                               draft->S, H, pl.draft_chunk, pl.n_suffix_chunks, pl.n_shared_chunks, sh->num_sms, softmax_scale, o_part_a, lse_part_a,
+                               draft->S, H, pl.draft_chunk, pl.n_suffix_chunks, pl.n_shared_chunks, sh->ckv, sh->kpe, (int)sh->Ls, sh->Ls_pad, pl.chunk,
+                               prefix_too ? pl.n_shared_chunks : 0, sh->num_sms, softmax_scale, o_part_a, lse_part_a,
                                forked ? nullptr : sh->w_uv};
             e = launch_draft_sm100(da, n_chunks == 1 ? o_lat : nullptr, lse_a, sh->status, s);
         }
@@ -1274,7 +1286,7 @@ int typhoon_mla_decode_draft(const typhoon_mla_shared_t* sh, const void* q_nope,
                            stream, false);
     const int rows = B * S;
     mode = resolve_mode(sh, rows, max_pages, mode);
-    const Plan pl = make_draft_plan(sh, cfg.naive_schedule, cfg.stacked_absorb, B, S, max_pages, page_size, mode);
+    const Plan pl = make_draft_plan(sh, cfg.naive_schedule, cfg.stacked_absorb, cache->ckv_exponents != nullptr, B, S, max_pages, page_size, mode);
     if (workspace_bytes < pl.total) return TYPHOON_MLA_ERR_WORKSPACE_TOO_SMALL;
     const DraftStep draft{cache, B, S, draft_lens, tree_mask};
     NaiveJob job{sh, 0, rows, pl.n_split_naive, pl.n_slots_naive, 0};

@@ -51,6 +51,7 @@ struct DraftParams {
     int B, S, H, rows;     // rows = S * H per request
     int row_tiles, chunk, n_chunks;
     int chunk0;            // partial slot of the first chunk
+    int Ls, sh_chunk, n_sh_chunks, n_sh_items;   // prefix items: 128 rows of the stacked [B * rows] matrix and a chunk of the prefix
     int page_size, max_pages, num_pages;
     const int32_t* block_table;
     const int32_t* seq_lens;
@@ -150,7 +151,8 @@ __device__ __forceinline__ float max_of(const float (&x)[N]) {
 template <bool E8>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<E8>::THREADS, 1)
 draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constant__ CUtensorMap tm_qp,
-                        const __grid_constant__ CUtensorMap tm_ckv, const __grid_constant__ CUtensorMap tm_kpe, DraftParams p) {
+                        const __grid_constant__ CUtensorMap tm_ckv, const __grid_constant__ CUtensorMap tm_kpe,
+                        const __grid_constant__ CUtensorMap tm_ckv_sh, const __grid_constant__ CUtensorMap tm_kpe_sh, DraftParams p) {
     using X = Shape<E8>;
     constexpr int KS = X::KS, VS = X::VS, LAT = X::LAT, HALF = LAT / 2, TPT = X::TPT, PARTS = X::PARTS, SM = 32 * X::WARPS;
     extern __shared__ uint8_t smem_raw[];
@@ -188,25 +190,32 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
     const uint32_t tmem_base = __shfl_sync(0xffffffffu, sh->tmem_base, 0);
     pdl_wait();
 
-    // Work items: row tile fastest (they share the tokens), then chunk, then request in longest-first order.  A pair takes every
+    // Work items: over the prefix (absorb-only steps of a 16-bit cache), chunk fastest, then 128 rows; over the suffixes, row tile
+    // fastest (they share the tokens), then chunk, then request in longest-first order.  A pair takes every
     // n_pairs-th, in alternating direction; what it loads for the next item starts when the logits of the last tile are there, beside
     // that tile's softmax, product and the item's epilogue.
     const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
-    const int n_items = p.row_tiles * p.n_chunks * p.B;
+    const int n_items = p.n_sh_items + p.row_tiles * p.n_chunks * p.B;
     const int64_t all_rows = (int64_t)p.B * p.rows;
     struct Item {
-        int b, tile, chunk, pg0, pg1;
+        int b, pg0, pg1;          // request (prefix items: -1)
+        int slot;                 // partial slot
+        int row0, n_rows;         // rows of the stacked matrix (n_rows 0: no item)
+        int tile;                 // ... of the request
         int tok_begin, tok_end, n_tiles, n_last;     // n_last: tokens of the last tile
         int draft0;               // first draft
         int first_special;        // tiles from this one on are gone through in shared memory before the second product
     };
     auto item_index = [&](int k) { return k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair); };
-    // {request, clamped suffix length, first two pages} of item k; length -1: no such item
+    // {request, clamped suffix length, first two pages} of item k; length -1: no such item, request -1: over the prefix
     auto desc_of = [&](int k) {
         const int i = item_index(k);
         int4 d = make_int4(0, -1, -1, -1);
-        if (i < n_items) {
-            const int z = i / (p.row_tiles * p.n_chunks);
+        if (i < p.n_sh_items) {
+            d.x = -1;
+            d.y = p.Ls;
+        } else if (i < n_items) {
+            const int z = (i - p.n_sh_items) / (p.row_tiles * p.n_chunks);
             if (p.desc != nullptr) d = p.desc[z];
             else d = make_int4(z, min(max(p.seq_lens[z], 0), p.max_pages * p.page_size), -1, -1);
         }
@@ -214,24 +223,30 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
     };
     auto item_at = [&](int k, int4 d) {
         Item it;
-        const int i = item_index(k);
         // (through shuffles: the role warps' loops are then known to be uniform)
         const int len = __shfl_sync(0xffffffffu, d.y, 0);
         it.b = __shfl_sync(0xffffffffu, d.x, 0);
         it.pg0 = d.z;
         it.pg1 = d.w;
-        it.tile = len < 0 ? -1 : i % p.row_tiles;
-        it.chunk = (i / p.row_tiles) % p.n_chunks;
-        it.tok_begin = it.chunk * p.chunk;
-        it.tok_end = min(max(len, 0), it.tok_begin + p.chunk);
+        const bool prefix = it.b < 0;
+        const int i = item_index(k) - (prefix ? 0 : p.n_sh_items);
+        const int tile = prefix ? i / p.n_sh_chunks : i % p.row_tiles;
+        const int chunk = prefix ? i % p.n_sh_chunks : (i / p.row_tiles) % p.n_chunks;
+        it.slot = prefix ? chunk : p.chunk0 + chunk;
+        it.row0 = (prefix ? 0 : it.b * p.rows) + tile * 128;
+        it.n_rows = len < 0 ? 0 : min(128, (prefix ? p.B * p.rows : p.rows) - tile * 128);
+        it.tile = tile;
+        it.tok_begin = chunk * (prefix ? p.sh_chunk : p.chunk);
+        it.tok_end = min(max(len, 0), it.tok_begin + (prefix ? p.sh_chunk : p.chunk));
         it.n_tiles = it.tok_end > it.tok_begin ? (it.tok_end - it.tok_begin + TOK - 1) / TOK : 0;
         it.n_last = it.tok_end - it.tok_begin - (it.n_tiles - 1) * TOK;
-        // (a single token that sees itself hides nothing: no draft)
-        const int n_draft = p.draft_lens != nullptr && it.n_tiles > 0 ? min(max(p.draft_lens[it.b], 0), p.S) : p.S;
-        it.draft0 = __shfl_sync(0xffffffffu, p.S == 1 && p.mask == nullptr ? len : len - n_draft, 0);
+        // (no drafts in the prefix; a single token that sees itself hides nothing)
+        const int n_draft = p.draft_lens != nullptr && it.n_tiles > 0 && !prefix ? min(max(p.draft_lens[it.b], 0), p.S) : p.S;
+        it.draft0 = __shfl_sync(0xffffffffu, prefix || (p.S == 1 && p.mask == nullptr) ? len : len - n_draft, 0);
         // values of drafts that are not finite are zeroed (see above), and the rest of the last group of tokens, which may hold anything
+        // (the handle's copy of the prefix is padded with zeros)
         it.first_special = it.draft0 >= it.tok_end ? it.n_tiles : max(it.draft0 - it.tok_begin, 0) / TOK;
-        if (it.n_tiles > 0 && it.n_last % X::GROUP != 0) it.first_special = min(it.first_special, it.n_tiles - 1);
+        if (it.n_tiles > 0 && it.n_last % X::GROUP != 0 && !prefix) it.first_special = min(it.first_special, it.n_tiles - 1);
         return it;
     };
     const int n_rounds = n_items > 0 ? (n_items + n_pairs - 1) / n_pairs : 0;
@@ -251,6 +266,11 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
     // physical page and slot of half `h` (64 tokens) of tile j; a half past the end reads as zeros
     auto page_of = [&](const Item& it, int j, int h, int& page, int& slot) {
         const int t0 = it.tok_begin + j * TOK + h * 64;
+        if (it.b < 0) {           // 64-token pages of the handle's copy
+            page = t0 / 64;
+            slot = 0;
+            return;
+        }
         slot = t0 % p.page_size;
         page = __shfl_sync(0xffffffffu, t0 < it.tok_end ? page_at(it, t0) : p.num_pages, 0);
     };
@@ -274,15 +294,17 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
             if (pf_k >= n_rounds) return;
             int page, slot;
             page_of(pf, pf_j, (int)rank, page, slot);
+            const CUtensorMap* tc = pf.b < 0 ? &tm_ckv_sh : &tm_ckv;
 #pragma unroll 1
-            for (int i = 0; i < HALF; ++i) tma_prefetch_4d_if(ld, &tm_ckv, 0, slot, 2 * i, page);
-            tma_prefetch_3d_if(ld, &tm_kpe, 0, slot, page);
+            for (int i = 0; i < HALF; ++i) tma_prefetch_4d_if(ld, tc, 0, slot, 2 * i, page);
+            tma_prefetch_3d_if(ld, pf.b < 0 ? &tm_kpe_sh : &tm_kpe, 0, slot, page);
             ++pf_j;
         };
         bool ok = true;
         int g = 0, n = 0;
         for (int k = 0; k < n_rounds && ok; ++k) {
             const Item it = item_at(k, desc_of(k));
+            const CUtensorMap* tc = it.b < 0 ? &tm_ckv_sh : &tm_ckv;
             for (int j = 0; j < it.n_tiles && ok; ++j, ++g) {
                 int page, slot;
                 page_of(it, j, (int)rank, page, slot);
@@ -295,15 +317,15 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                     const uint32_t kf = cluster_map(&sh->k_full[s][h], 0);
                     mbar_arrive_expect_tx_if(ld_even, &sh->k_full[s][h], 2 * (HALF + h) * SLAB);
 #pragma unroll
-                    for (int i = 0; i < HALF; i += 2) tma_load_4d_pair_if(ld, dst + i * SLAB, &tm_ckv, kf, 0, slot, HALF * h + i, page);
-                    if (h == 1) tma_load_3d_pair_if(ld, dst + HALF * SLAB, &tm_kpe, kf, 0, slot, page);
+                    for (int i = 0; i < HALF; i += 2) tma_load_4d_pair_if(ld, dst + i * SLAB, tc, kf, 0, slot, HALF * h + i, page);
+                    if (h == 1) tma_load_3d_pair_if(ld, dst + HALF * SLAB, it.b < 0 ? &tm_kpe_sh : &tm_kpe, kf, 0, slot, page);
                 }
                 issued = g + 1;
                 if (j == 0 && ok) {
                     if (n > 0) ok = mbar_wait_warp(&sh->q_empty, (n - 1) & 1, abort_flag);
                     if (!ok) break;
                     const uint32_t qf = cluster_map(&sh->q_full, 0);
-                    const int y = it.b * p.rows + it.tile * 128 + 64 * (int)rank;
+                    const int y = it.row0 + 64 * (int)rank;
                     mbar_arrive_expect_tx_if(ld_even, &sh->q_full, 2 * X::Q_BYTES);
 #pragma unroll 1
                     for (int sl = 0; sl < 8; ++sl) tma_load_2d_pair_if(ld, sQ + sl * SLAB, &tm_qa, qf, sl * 64, y);
@@ -327,6 +349,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
         int g = 0;
         for (int k = 0; k < n_rounds && ok; ++k) {
             const Item it = item_at(k, desc_of(k));
+            const CUtensorMap* tc = it.b < 0 ? &tm_ckv_sh : &tm_ckv;
             for (int j = 0; j < it.n_tiles && ok; ++j, ++g) {
                 int page[2], slot[2];
                 page_of(it, j, 0, page[0], slot[0]);
@@ -345,8 +368,8 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                     const uint32_t bar = special ? (st ? vt[1] : vt[0]) : (i ? vf[1] : vf[0]);
                     // 16 bits: blocks of 128 dims, [block][token half][2 slabs]; 8 bits: [token half][2 slabs = blocks]
                     const int slab = E8 ? 2 * (int)rank : 4 * (int)rank + 2 * nb;
-                    tma_load_4d_pair_if(ld, dst + (4 * nb) * SLAB, &tm_ckv, bar, 0, slot[0], slab, page[0]);
-                    tma_load_4d_pair_if(ld, dst + (4 * nb + 2) * SLAB, &tm_ckv, bar, 0, slot[1], slab, page[1]);
+                    tma_load_4d_pair_if(ld, dst + (4 * nb) * SLAB, tc, bar, 0, slot[0], slab, page[0]);
+                    tma_load_4d_pair_if(ld, dst + (4 * nb + 2) * SLAB, tc, bar, 0, slot[1], slab, page[1]);
                 }
                 if (special) ++issued_t[st];
                 else ++issued_v[st];
@@ -483,9 +506,9 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
         for (int k = 0; k < n_rounds; ++k) {
             const Item it = item_at(k, next);
             next = desc_of(k + 1);        // (asked for an item ahead)
-            if (it.tile < 0) continue;
-            const int n_rows = min(128, p.rows - it.tile * 128);
-            const int64_t row0 = (int64_t)it.b * p.rows + it.tile * 128;
+            if (it.n_rows == 0) continue;
+            const int n_rows = it.n_rows;
+            const int64_t row0 = it.row0;
             if (it.n_tiles == 0) {
                 // empty chunk: weight zero in the merge (a request without any latent token: zero latent output)
                 const int r = 64 * (int)rank + (int)threadIdx.x - 128;
@@ -495,7 +518,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                         for (int l = 0; l < 512; l += 8)
                             *reinterpret_cast<uint4*>(p.o_lat_direct + (row0 + r) * 512 + l) = make_uint4(0, 0, 0, 0);
                     } else {
-                        p.lse_part[(p.chunk0 + it.chunk) * all_rows + row0 + r] = -INFINITY;
+                        p.lse_part[(int64_t)it.slot * all_rows + row0 + r] = -INFINITY;
                     }
                 }
                 continue;
@@ -503,8 +526,8 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
             const bool mine = 64 * (int)rank + row < n_rows;      // (else nobody's: sees nothing)
             uint64_t sees = 0;            // bit i: draft i
             if (mine) {
-                const int j = (it.tile * 128 + 64 * (int)rank + row) / p.H;
-                sees = p.mask != nullptr ? p.mask[(int64_t)it.b * p.S + j] : (2ull << j) - 1ull;
+                const int j = (it.tile * 128 + 64 * (int)rank + row) / p.H;      // (unused over the prefix)
+                sees = it.b >= 0 && p.mask != nullptr ? p.mask[(int64_t)it.b * p.S + j] : (2ull << (j & 63)) - 1ull;
             }
             const float tau = E8 && mine ? p.q_tau[row0 + 64 * (int)rank + row] : 1.f;
             float m_ref = -INFINITY;      // log2 units; 8 bits: of the logits times the tokens' powers of two
@@ -767,7 +790,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                 const float lse = l == 0.f ? -INFINITY : l == l ? (m + log2f(l)) * kLn2 : kLseNotFinite;
                 const int64_t r = row0 + 64 * (int)rank + row;
                 if (direct) p.lse_direct[r] = lse;
-                else p.lse_part[(p.chunk0 + it.chunk) * all_rows + r] = lse;
+                else p.lse_part[(int64_t)it.slot * all_rows + r] = lse;
             }
             if (vote_or<SM>(*abort_flag != 0 || !mbar_wait(&sh->o_done[(g - 1) & 1], ((g - 1) >> 1) & 1, abort_flag))) break;
             tc_fence_after();
@@ -793,7 +816,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                         store_sector(dst + 16 * c, v);
                     }
                 } else {
-                    float* dst = p.o_part + ((int64_t)(p.chunk0 + it.chunk) * all_rows + r) * 512 + col0 + 32 * i;
+                    float* dst = p.o_part + ((int64_t)it.slot * all_rows + r) * 512 + col0 + 32 * i;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         uint32_t v[8];
@@ -900,7 +923,8 @@ cudaError_t launch_draft_sm100(const DraftAttn& a, void* o_lat_direct, float* ls
     const bool e8 = a.cache->ckv_exponents != nullptr;
     const int rows = a.S * a.H;
     const int64_t all_rows = (int64_t)a.B * rows;
-    CUtensorMap tm_qa, tm_qp, tm_ckv, tm_kpe;
+    if (a.n_sh_chunks > 0 && (e8 || a.sh_chunk % TOK != 0)) return cudaErrorInvalidValue;
+    CUtensorMap tm_qa, tm_qp, tm_ckv, tm_kpe, tm_ckv_sh, tm_kpe_sh;
     uint32_t box[2] = {64, 64};
     {   // the queries as one matrix of 1 KB rows (512 values, or both terms of 512); rows past the end read as zeros
         uint64_t dims[2] = {512, (uint64_t)all_rows};
@@ -914,6 +938,13 @@ cudaError_t launch_draft_sm100(const DraftAttn& a, void* o_lat_direct, float* ls
     }
     cudaError_t e = make_kv_tmaps(*a.cache, &tm_ckv, &tm_kpe);
     if (e != cudaSuccess) return e;
+    tm_ckv_sh = tm_ckv;
+    tm_kpe_sh = tm_kpe;
+    if (a.n_sh_chunks > 0) {
+        const typhoon_mla_cache_t prefix{const_cast<void*>(a.ckv_shared), const_cast<void*>(a.kpe_shared), nullptr, 512, 64, 64, (int32_t)(a.Ls_pad / 64)};
+        e = make_kv_tmaps(prefix, &tm_ckv_sh, &tm_kpe_sh);
+        if (e != cudaSuccess) return e;
+    }
     DraftParams p{};
     p.B = a.B; p.S = a.S; p.H = a.H; p.rows = rows;
     p.row_tiles = (rows + 127) / 128; p.chunk = a.chunk; p.n_chunks = a.n_chunks; p.chunk0 = a.chunk0;
@@ -924,14 +955,17 @@ cudaError_t launch_draft_sm100(const DraftAttn& a, void* o_lat_direct, float* ls
     p.o_part = a.o_part; p.lse_part = a.lse_part;
     p.o_lat_direct = static_cast<__nv_bfloat16*>(o_lat_direct); p.lse_direct = lse_direct; p.status = status;
     p.q_tau = a.q_tau; p.exponents = a.cache->ckv_exponents;
-    const int64_t items = (int64_t)p.row_tiles * a.n_chunks * a.B;
+    p.Ls = a.Ls; p.sh_chunk = a.sh_chunk; p.n_sh_chunks = a.n_sh_chunks;
+    const int64_t sh_items = a.n_sh_chunks * ((all_rows + 127) / 128);
+    const int64_t items = sh_items + (int64_t)p.row_tiles * a.n_chunks * a.B;
     if (items > INT32_MAX / 2) return cudaErrorInvalidValue;
+    p.n_sh_items = (int)sh_items;
     p.l2_base = static_cast<const char*>(a.w_uv);
     p.l2_total = a.w_uv ? (uint32_t)a.H * 128u * 512u * 2u : 0u;
     const int pairs = (int)std::min<int64_t>(items, std::max(a.n_sm / 2, 1));
     p.l2_bytes = (p.l2_total / (pairs * 32u) / 16u + 1u) * 16u;
     auto* kernel = e8 ? draft_pair_sm100_kernel<true> : draft_pair_sm100_kernel<false>;
-    return launch_pdl(kernel, dim3((unsigned)(2 * pairs)), dim3(e8 ? Shape<true>::THREADS : Shape<false>::THREADS), kDraftSmem, s, tm_qa, tm_qp, tm_ckv, tm_kpe, p);
+    return launch_pdl(kernel, dim3((unsigned)(2 * pairs)), dim3(e8 ? Shape<true>::THREADS : Shape<false>::THREADS), kDraftSmem, s, tm_qa, tm_qp, tm_ckv, tm_kpe, tm_ckv_sh, tm_kpe_sh, p);
 }
 
 }  // namespace tmla

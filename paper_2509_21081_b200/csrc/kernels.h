@@ -234,6 +234,8 @@ struct DraftAttn {
     const uint64_t* mask;                          // optional [B,S]: bit i, draft i is visible to the row (else 0 .. j to row j)
     const int32_t* desc;                           // optional [B][4]: per launch position, see launch_q_absorb_sm100
     int B, S, H; int chunk, n_chunks, chunk0;
+    // absorb-only steps of a 16-bit cache: the prefix as well, in slots [0, n_sh_chunks) (sh_chunk a multiple of 128)
+    const void* ckv_shared; const void* kpe_shared; int Ls; int64_t Ls_pad; int sh_chunk, n_sh_chunks;
     int n_sm;
     float scale;
     float* o_part;   // [slots][B*S][H][512], each normalised
