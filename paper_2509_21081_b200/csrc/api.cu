@@ -1108,21 +1108,39 @@ static int decode_core(const Settings& cfg, const typhoon_mla_shared* sh, const 
         prof_before(TYPHOON_MLA_KERNEL_ABSORB_ATTN, s);
         // (the kernel of drafted tokens takes the suffixes, and over a 16-bit cache the prefix of an absorb-only step as well)
         const bool prefix_too = draft && !draft->cache->ckv_exponents;
-        if (draft && (pl.n_shared_chunks == 0 || prefix_too)) e = cudaSuccess;
+        const bool two_kernels = draft && pl.n_shared_chunks > 0 && !prefix_too;
+        // Over an 8-bit cache the two kernels of an absorb-only step run side by side: the suffixes on the handle's stream.
+        // (B200, us per step, one behind the other / side by side: 1 request, 128 heads, 4859 + 35 tokens 47 / 34;
+        // 1 request of 8 drafts, 32 heads, 2540 + 316 tokens 58 / 32.)
+        const bool beside = two_kernels && cfg.overlap && sh->side_stream != nullptr;
+        if (beside) {
+            e = cudaEventRecord(sh->ev_fork, s);
+            if (e == cudaSuccess) e = cudaStreamWaitEvent(sh->side_stream, sh->ev_fork, 0);
+            if (e != cudaSuccess) return fail(e);
+            open_fork = true;
+        }
+        if (draft) {
+            const DraftAttn da{q_terms ? q_terms : q_abs, q_pe, q_tau, draft->cache, block_table, max_pages, seq_lens, draft->draft_lens, draft->mask,
+                               desc, draft->n_requests, draft->S, H, pl.draft_chunk, pl.n_suffix_chunks, pl.n_shared_chunks, sh->ckv, sh->kpe,
+                               (int)sh->Ls, sh->Ls_pad, pl.chunk, prefix_too ? pl.n_shared_chunks : 0, sh->num_sms, softmax_scale, o_part_a,
+                               lse_part_a, forked || two_kernels ? nullptr : sh->w_uv};
+            e = launch_draft_sm100(da, n_chunks == 1 ? o_lat : nullptr, lse_a, sh->status, beside ? sh->side_stream : s);
+            if (e != cudaSuccess) return fail(e);
+            if (two_kernels) ++launches;
+        }
+        if (draft && !two_kernels) e = cudaSuccess;
         else if (!tc) e = launch_absorb_attn_mma(ab, s);
         else if (pl.absorb_pairs) e = launch_absorb_pair_sm100(ab, sh->Ls_pad, o_lat, lse_a, sh->status, s);
         else e = launch_absorb_attn_sm100(ab, &sh->tm_ckv, &sh->tm_kpe_tok, o_lat, lse_a, sh->status, s);
-        if (draft && e == cudaSuccess) {
-            if (pl.n_shared_chunks > 0 && !prefix_too) ++launches;
-            const DraftAttn da{q_terms ? q_terms : q_abs, q_pe, q_tau, draft->cache, block_table, max_pages, seq_lens, draft->draft_lens, draft->mask, desc, draft->n_requests,
-                               draft->S, H, pl.draft_chunk, pl.n_suffix_chunks, pl.n_shared_chunks, sh->ckv, sh->kpe, (int)sh->Ls, sh->Ls_pad, pl.chunk,
-                               prefix_too ? pl.n_shared_chunks : 0, sh->num_sms, softmax_scale, o_part_a, lse_part_a,
-                               forked ? nullptr : sh->w_uv};
-            e = launch_draft_sm100(da, n_chunks == 1 ? o_lat : nullptr, lse_a, sh->status, s);
-        }
         prof_after(TYPHOON_MLA_KERNEL_ABSORB_ATTN, s);
         if (e != cudaSuccess) return fail(e);
         ++launches;
+        if (beside) {
+            e = cudaEventRecord(sh->ev_join, sh->side_stream);
+            if (e == cudaSuccess) e = cudaStreamWaitEvent(s, sh->ev_join, 0);
+            open_fork = false;
+            if (e != cudaSuccess) return cuda_fail(e);
+        }
         if (n_jobs == 0 && n_empties == 0 && n_chunks > 1 && (int64_t)B * H <= sh->num_sms) {
             // Absorb-only with at most one (request, head) row per SM: merge + projection + rounding in one launch, a block
             // per row (one block fills an SM's registers).  Measured (B200, us per step, this form / merge and GEMM): 16

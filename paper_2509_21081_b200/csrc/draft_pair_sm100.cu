@@ -961,8 +961,9 @@ cudaError_t launch_draft_sm100(const DraftAttn& a, void* o_lat_direct, float* ls
     if (items > INT32_MAX / 2) return cudaErrorInvalidValue;
     p.n_sh_items = (int)sh_items;
     p.l2_base = static_cast<const char*>(a.w_uv);
-    p.l2_total = a.w_uv ? (uint32_t)a.H * 128u * 512u * 2u : 0u;
     const int pairs = (int)std::min<int64_t>(items, std::max(a.n_sm / 2, 1));
+    // (4 KB per lane at most: a few pairs that ask for all of it would wait behind it themselves; 1 request x 128 heads 63 -> 47 us a step)
+    p.l2_total = a.w_uv ? (uint32_t)std::min<int64_t>((int64_t)a.H * 128 * 512 * 2, (int64_t)pairs * 32 * 4096) : 0u;
     p.l2_bytes = (p.l2_total / (pairs * 32u) / 16u + 1u) * 16u;
     auto* kernel = e8 ? draft_pair_sm100_kernel<true> : draft_pair_sm100_kernel<false>;
     return launch_pdl(kernel, dim3((unsigned)(2 * pairs)), dim3(e8 ? Shape<true>::THREADS : Shape<false>::THREADS), kDraftSmem, s, tm_qa, tm_qp, tm_ckv, tm_kpe, tm_ckv_sh, tm_kpe_sh, p);
