@@ -463,7 +463,8 @@ int typhoon_mla_cache_read(const typhoon_mla_cache_t* cache /* host */, const in
  *   block_table int32 [B, max_pages], seq_lens int32 [B]: per request (max_pages >= 1); bad page ids as in typhoon_mla_decode
  *   mode  AUTO, ABSORB or HYBRID (NAIVE: INVALID_ARG)
  *   workspace  typhoon_mla_draft_workspace_bytes, which also serves every step of fewer requests, fewer drafts or a narrower table
- * With an 8-bit cache the latent values are what the codes stand for; computation is as exact as over a 16-bit cache.
+ * With an 8-bit cache the latent values are what the codes stand for; computation is as exact as over a 16-bit cache (values below
+ * 2^-90 of magnitude count as zeros in the output).
  * B * S <= TYPHOON_MLA_MAX_DRAFT_ROWS; tcgen05 kernel path only (UNSUPPORTED_DIMS otherwise); streams, capture and errors as
  * typhoon_mla_decode.
  */

@@ -24,7 +24,8 @@
 // The rope part (16-bit, unscaled) goes to an accumulator of its own, and a logit is S_lat * 2^(tau + e_t) + S_rope.  The token's power
 // of two belongs to its values as well: with x the scaled logit in log2 units P = 2^(x + e_t - n) against a reference n of the x + e_t,
 // while the row sum is of 2^(x - m) against a reference m of the x (per thread; any within 2^40 will do in 32 bits):
-// P = 2^(x - m) * 2^e_t * kappa with kappa = 2^(m - n) per thread and tile.
+// P = 2^(x - m) * 2^e_t * kappa with kappa = 2^(m - n) per thread and tile.  n is kept within 2^100 of the largest weight (and of the
+// largest power of two), where kappa is a normal number: tokens whose values are under 2^-100 next to their weight count as zeros.
 //
 // (Query absorption splits Q, from 32 bits; the split of P is here, from 32 bits as well.)
 //
@@ -45,6 +46,7 @@ using namespace sm100;
 constexpr int TOK = 128;
 constexpr int SLAB = 64 * 128;                   // [64 rows][128 bytes], swizzled
 constexpr float kLog2Off = 4.f, kLog2Room = 4.f; // 8 bits: P at the reference is 2^4, and at most 2^4 times that
+constexpr float kLog2Floor = 100.f;              // 8 bits: references are no further below the largest weight than this
 constexpr float kRescale16 = 8.f;                // 16 bits: log2 above the reference
 
 struct DraftParams {
@@ -629,15 +631,18 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                             for (int c = 0; c < TPT; ++c) x[c] -= top;
                             top = 0.f;
                         }
-                        kappa = m_ref == -INFINITY ? 0.f : fast_exp2(m_sum - m_ref + kLog2Off);
-                        // some 2^x sigma kappa above its limit?  First by the largest of both factors.
-                        exceed = m_ref == -INFINITY ? top != -INFINITY : fast_exp2(top) * (max_of(sigma) * kappa) > 256.f;     // 2^(kLog2Off + kLog2Room)
+                        kappa = m_ref == -INFINITY ? 0.f : fast_exp2(fminf(m_sum - m_ref + kLog2Off, 120.f));
+                        // some 2^x sigma kappa above its limit?  First by the largest of both factors.  (And kappa, with or without a
+                        // power of two, stays far from what 32 bits hold.)
+                        const float most_k = max_of(sigma) * kappa;
+                        exceed = m_ref == -INFINITY ? top != -INFINITY : fast_exp2(top) * most_k > 256.f;     // 2^(kLog2Off + kLog2Room)
                         if (exceed && m_ref != -INFINITY) {
                             float most = 0.f;
 #pragma unroll
                             for (int c = 0; c < TPT; ++c) most = fmaxf(most, fast_exp2(x[c]) * (sigma[E8 ? c : 0] * kappa));
                             exceed = most > 256.f;
                         }
+                        exceed |= fmaxf(most_k, kappa) > 0x1p105f;
                     } else {
                         // (a row without a reference: any logit exceeds it)
                         exceed = top > (m_ref == -INFINITY ? -INFINITY : kRescale16);
@@ -652,7 +657,12 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
 #pragma unroll
                         for (int c = 0; c < TPT; ++c)
                             if (sigma[E8 ? c : 0] > 0.f) most = fmaxf(most, x[c] + (float)((int)(__float_as_uint(sigma[E8 ? c : 0]) >> 23) - 127));
-                        top = most + (m_sum == -INFINITY ? 0.f : m_sum);
+                        // (at least 2^-kLog2Floor of the largest weight and of the largest power of two seen beside it: what is below
+                        // counts as nothing)
+                        const float sum_ref = m_sum == -INFINITY ? 0.f : m_sum, most_s = max_of(sigma);
+                        if (top != -INFINITY)
+                            most = fmaxf(most, fmaxf(top, 0.f) - kLog2Floor + (most_s > 1.f ? (float)((int)(__float_as_uint(most_s) >> 23) - 127) : 0.f));
+                        top = most + sum_ref;
                     } else {
                         top += base;
                     }
@@ -688,7 +698,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                     }
                     if (ok) {
                         if (E8) {
-                            kappa = m_ref == -INFINITY ? 0.f : fast_exp2(m_sum - m_ref + kLog2Off);
+                            kappa = m_ref == -INFINITY ? 0.f : fast_exp2(fminf(m_sum - m_ref + kLog2Off, 120.f));
                         } else {
                             const float d = base - (m_ref == -INFINITY ? 0.f : m_ref);
 #pragma unroll

@@ -131,6 +131,32 @@ def test_8_bit_tokens_of_different_sizes(b, spread, peak):
     check(got, want, lse, want_lse, tensor_tol=5e-3 * size, row_tol=4 * 2.0 ** -8 * size)
 
 
+def test_8_bit_rows_of_zeros_and_extreme_exponents(b):
+    """Rows of zeros as they are written here (byte 1, 2^-126), alone and among others, also where one of them takes nearly all the
+    weight; powers of two up to 2^100 apart; bytes 0.  The row sums have all of them, the output what is not negligible."""
+    H, S = 16, 2
+    p = Problem(H, S, 0, [40, 200, 131, 200, 140, 300], bits=8, seed=21)
+    codes, ex, kpe = p.ckv_pages.view(-1, 512), p.exponents.view(-1), p.kpe_pages.view(-1, 64)
+    codes[p.slot[0]], ex[p.slot[0]] = 0, 1                                 # nothing but zeros
+    codes[p.slot[1][::3]], ex[p.slot[1][::3]] = 0, 1                       # zeros among others
+    at = p.slot[2][100]
+    codes[at], ex[at] = 0, 1
+    kpe[at] = 40.0 * torch.sign(p.q_pe[2 * S, 0].float()).to(torch.bfloat16)     # a row of zeros that is worth 2^150 of the others for one row
+    ex[p.slot[3][50:60]] = 200                                             # values of 2^70 and more: their logits decide
+    ex[p.slot[4]] = torch.randint(20, 110, (140,), dtype=torch.uint8)      # down to 2^-107
+    codes[p.slot[5][7]], ex[p.slot[5][7]] = 0, 0
+    got, lse, status = p.step()
+    assert status == 0 and torch.isfinite(got).all() and not got[:S].any()
+    want, want_lse = p.reference()
+    rows = [r for r in range(12) if r // S not in (2, 3)]
+    check(got[rows], want[rows], lse[rows], want_lse[rows])
+    # one row per head may be all weight on a row of zeros: nothing there but what is below 2^-90
+    big = want[4:6].norm(dim=-1) > 1e-3
+    off = (got[4:6] - want[4:6]).norm(dim=-1)
+    assert (off[big] <= 4 * 2.0 ** -8 * want[4:6].norm(dim=-1)[big]).all() and (off[~big] <= 1e-5).all()
+    assert (lse[4:6] - want_lse[4:6]).abs().max().item() <= 2e-2 * max(1.0, float(want_lse[4:6].abs().max()) / 10)
+
+
 def test_8_and_16_bits_agree(b):
     """The same values in either cache: the two kernels differ by their roundings alone."""
     p = Problem(128, 2, 500, [640, 100, 333], bits=8, seed=9, poison=False)
