@@ -369,8 +369,10 @@ Plan make_draft_plan(const typhoon_mla_shared* sh, int schedule, bool stacked, b
     Plan p{};
     p.mode = mode;
     if (mode != TYPHOON_MLA_MODE_ABSORB && sh->Ls > 0) {
-        // SM time of the absorb branch beside it (as absorb_branch_us, with row_tiles items per request)
-        const double beside = 4.0 * H * ((Q + 127) / 128) + 2.0 * B * row_tiles * (10.0 + 1.25 * (double)tiles);
+        // SM time of the absorb branch beside it (us).  A pair works on an item 4 us and 1.3 per tile; the table holds about twice what
+        // the suffixes do.  (B200, us per step, with absorb_branch_us's constants / these: 83 requests x 2 x 16 heads, 7069 + 3..1537
+        // tokens 61.6 / 57.4; 146 x 2 x 16, 766 + 25..35 45 / 38; 13 x 16 x 128, 1562 + 51..61 120 / 104; 11 others 0.98-1.08 times as fast.)
+        const double beside = 1.6 * H * ((Q + 127) / 128) + 2.0 * B * row_tiles * (4.0 + 0.5 * (double)tiles);
         const int max_slots = (int)std::min<int64_t>(floor_slot_rows(n_sm, rows, sh->Ls) / rows, INT32_MAX);
         naive_sm100_plan(Q, H, sh->Ls, naive_places(Q, n_sm, sh->fp8 != 0), schedule, &p.n_split_naive, &p.n_slots_naive, sh->fp8 != 0, beside,
                          max_slots);
