@@ -540,7 +540,7 @@ int typhoon_mla_set_absorb_efficiency(double fraction) {
 // 48 over 512 tokens 49.9 against 45.7).
 constexpr double kNaiveTime8Bit = 1.3;
 static int choose_mode_impl(const typhoon_mla_dims_t* dims, int64_t Ls, int32_t B, int64_t total_suffix_tokens,
-                            double naive_time_factor) {
+                            double naive_time_factor, double absorb_fixed_s = 0.0) {
     if (!dims || B < 1 || Ls <= 0) return TYPHOON_MLA_MODE_ABSORB;
     if (total_suffix_tokens == 0) return TYPHOON_MLA_MODE_NAIVE;
     // Shared-prefix part only: the suffix part is identical in both modes.
@@ -561,7 +561,7 @@ static int choose_mode_impl(const typhoon_mla_dims_t* dims, int64_t Ls, int32_t 
     // further from the 64-bit one (3.0e-3 against 2.2e-3).  A caller can ask for it.
     const double T = g_tensor_flops.load(), M = g_hbm_bytes.load();
     const double t_hybrid = naive_time_factor * std::max(f_naive / T, by_naive / M) + g_hybrid_fixed_s.load();
-    const double t_absorb = std::max(f_absorb / (g_absorb_efficiency.load() * T), by_absorb / M);
+    const double t_absorb = std::max(f_absorb / (g_absorb_efficiency.load() * T), by_absorb / M) + absorb_fixed_s;
     return t_hybrid < t_absorb ? TYPHOON_MLA_MODE_HYBRID : TYPHOON_MLA_MODE_ABSORB;
 }
 
@@ -1305,6 +1305,11 @@ int typhoon_mla_decode_draft(const typhoon_mla_shared_t* sh, const void* q_nope,
                            cache->num_pages, block_table, max_pages, seq_lens, softmax_scale, mode, out, lse_out, workspace, workspace_bytes,
                            stream, false);
     const int rows = B * S;
+    // Over an 8-bit cache an absorb-only step has a kernel for the suffixes beside the one for the prefix, and two streams to join.  (B200,
+    // us per step, absorb-only / hybrid: 96 requests x 16 heads, 277 + 26..67 tokens 45 / 32; 110 x 64, 226 + 408..1908 95 / 81; 8 x 3 x
+    // 128, 891 + 108..130 53 / 46; on the other side 8 x 2 x 128, 1775 + 221..437 53 / 62; 6 x 128, 1442 + 4..89 47 / 50.)
+    if (mode == TYPHOON_MLA_MODE_AUTO)
+        mode = choose_mode_impl(&sh->dims, sh->Ls, rows, -1, sh->fp8 ? kNaiveTime8Bit : 1.0, cache->ckv_exponents ? 4.7e-6 : 0.0);
     mode = resolve_mode(sh, rows, max_pages, mode);
     const Plan pl = make_draft_plan(sh, cfg.naive_schedule, cfg.stacked_absorb, cache->ckv_exponents != nullptr, B, S, max_pages, page_size, mode);
     if (workspace_bytes < pl.total) return TYPHOON_MLA_ERR_WORKSPACE_TOO_SMALL;
