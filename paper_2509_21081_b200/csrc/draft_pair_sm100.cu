@@ -776,6 +776,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
             }
 
             // ---------------- epilogue: row sums, normalised partial, LSE
+            softmax_sync<SM>();     // (the last tile may have had a new reference: its maxima are read before the sums take their place)
             sh->red[part][row] = l_part[0] + l_part[1];
             if (E8) sh->red2[E8 ? part : 0][E8 ? row : 0] = m_sum;
             softmax_sync<SM>();
