@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(512) merge_latent_kernel(const float* __restri
     // maximum of the chunk LSEs
     float m = -INFINITY;
     for (int c = tid; c < n_chunks; c += nthr) {
-        const float l = lse_part[(int64_t)c * BH + bh];
+        const float l = partial_lse(lse_part[(int64_t)c * BH + bh]);
         w_s[c] = l;
         m = fmaxf(m, l);
     }
@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(512) merge_latent_few_kernel(const float* __re
     float l[NC];
     float4 v[NC];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) l[c] = c < n_chunks ? lse_part[(int64_t)c * BH + bh] : -INFINITY;
+    for (int c = 0; c < NC; ++c) l[c] = c < n_chunks ? partial_lse(lse_part[(int64_t)c * BH + bh]) : -INFINITY;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
         v[c] = c < n_chunks ? *reinterpret_cast<const float4*>(o_part + ((int64_t)c * BH + bh) * 512 + col * 4)
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(512, 1) merge_project_kernel(const float* __re
     const float* src = o_part + (int64_t)bh * 512 + col * 4;
     const int64_t step = (int64_t)BH * 512;
     const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l0 = tid < n_chunks ? lse_part[(int64_t)tid * BH + bh] : -INFINITY;
+    float l0 = tid < n_chunks ? partial_lse(lse_part[(int64_t)tid * BH + bh]) : -INFINITY;
     float4 v[MP_BATCH];
 #pragma unroll
     for (int i = 0; i < MP_BATCH; ++i) {
@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(512, 1) merge_project_kernel(const float* __re
     float m = l0;
     w_s[tid] = l0;
     for (int c = tid + 512; c < n_chunks; c += 512) {
-        const float l = lse_part[(int64_t)c * BH + bh];
+        const float l = partial_lse(lse_part[(int64_t)c * BH + bh]);
         w_s[c] = l;
         m = fmaxf(m, l);
     }
@@ -268,17 +268,17 @@ __global__ void __launch_bounds__(256) combine_kernel(const float* __restrict__ 
     const int lane = threadIdx.x & 31;
     if (bh >= BH) return;
     float m = -INFINITY;
-    for (int i = 0; i < n_naive; ++i) m = fmaxf(m, lse_naive[(int64_t)i * BH + bh]);
+    for (int i = 0; i < n_naive; ++i) m = fmaxf(m, partial_lse(lse_naive[(int64_t)i * BH + bh]));
     float la = -INFINITY;
     if (o_abs != nullptr) {
-        la = lse_abs[bh];
+        la = partial_lse(lse_abs[bh]);
         m = fmaxf(m, la);
     }
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float z = 0.f;
     if (m != -INFINITY) {
         for (int i = 0; i < n_naive; ++i) {
-            float l = lse_naive[(int64_t)i * BH + bh];
+            float l = partial_lse(lse_naive[(int64_t)i * BH + bh]);
             if (l == -INFINITY) continue;
             float w = __expf(l - m);
             float4 v = *reinterpret_cast<const float4*>(o_naive + ((int64_t)i * BH + bh) * 128 + lane * 4);
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(256) combine_kernel(const float* __restrict__ 
         uint2 pk = make_uint2(pack_bf16(acc.x, acc.y), pack_bf16(acc.z, acc.w));
         *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(out) + (int64_t)bh * 128 + lane * 4) = pk;
     }
-    if (lse_out != nullptr && lane == 0) lse_out[bh] = (m == -INFINITY) ? -INFINITY : m + __logf(z);
+    if (lse_out != nullptr && lane == 0) lse_out[bh] = (m == -INFINITY) ? -INFINITY : merged_lse(m, z);
 }
 
 // What a prepared prefix keeps besides the expansion (see launch_prepare_layout), one launch of three kinds of blocks.  Bound

@@ -17,6 +17,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 // LSE by which a partial of drafted tokens says that some logit of the row is not finite: its weight in any merge is 1 and its values
 // are NaN, so the row becomes NaN.
 constexpr float kLseNotFinite = 3.2e38f;
+// (a kernel's own LSE of such a row may also be a NaN: the merges take it as this)
+__device__ __forceinline__ float partial_lse(float l) { return l == l ? l : kLseNotFinite; }
 // LSE of a row from the largest of its partials' and the sum of their weights (m > -inf).
 __device__ __forceinline__ float merged_lse(float m, float z) { return m < kLseNotFinite ? m + __logf(z) : __int_as_float(0x7fc00000); }
 

@@ -203,10 +203,10 @@ project_sm100_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
             // merge weights of this (request, head)
             float la = -INFINITY, m = -INFINITY;
             if (live) {
-                la = ce.lse_abs[bh];
+                la = partial_lse(ce.lse_abs[bh]);
                 m = la;
 #pragma unroll 4
-                for (int i = 0; i < p.n_slots; ++i) m = fmaxf(m, ce.lse_naive[i * BH + bh]);
+                for (int i = 0; i < p.n_slots; ++i) m = fmaxf(m, partial_lse(ce.lse_naive[i * BH + bh]));
             }
             const float wa = (la == -INFINITY) ? 0.f : __expf(la - m);
             float zsum = wa;
@@ -216,7 +216,7 @@ project_sm100_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
             // weighted sum of the slots, while the product is running
 #pragma unroll 1
             for (int i = 0; i < p.n_slots && ok; ++i) {
-                const float l = live ? ce.lse_naive[i * BH + bh] : -INFINITY;
+                const float l = live ? partial_lse(ce.lse_naive[i * BH + bh]) : -INFINITY;
                 const float w = (l == -INFINITY) ? 0.f : __expf(l - m);   // an empty partial's slot was never written
                 zsum += w;
 #pragma unroll
@@ -363,7 +363,7 @@ project_latency_sm100_kernel(const __grid_constant__ CUtensorMap tmA, const __gr
         float4 v[LAT_BN / 4];
         float wa = 0.f, wn = 0.f, inv = 0.f, lse = -INFINITY;
         if (live) {
-            const float la = ce.lse_abs[bh], ln = p.n_slots > 0 ? ce.lse_naive[bh] : -INFINITY;
+            const float la = partial_lse(ce.lse_abs[bh]), ln = p.n_slots > 0 ? partial_lse(ce.lse_naive[bh]) : -INFINITY;
             const float m = fmaxf(la, ln);
             wa = (la == -INFINITY) ? 0.f : __expf(la - m);
             wn = (ln == -INFINITY) ? 0.f : __expf(ln - m);      // (an empty partial's slot was never written)

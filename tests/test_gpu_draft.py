@@ -358,5 +358,52 @@ def test_refusals(b):
              out=torch.empty_like(q65))
     assert b.typhoon_mla_draft_workspace_bytes(dec.shared, 2, 65, 2, 64) == 0
     assert b.typhoon_mla_draft_workspace_bytes(dec.shared, 2, 2, 0, 64) == 0
+    assert b.typhoon_mla_draft_workspace_bytes(dec.shared, 2, 2, (1 << 23) + 1, 64) == 0 < b.typhoon_mla_draft_workspace_bytes(dec.shared, 2, 2, 1 << 23, 128)
     assert b.typhoon_mla_draft_workspace_bytes(dec.shared, 2, 2, 2, 32) == 0
     assert b.typhoon_mla_draft_workspace_bytes(dec.shared, 2, 2, 2, 64, 3) == 0
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("mode", ["absorb", "hybrid"])
+@pytest.mark.parametrize("H,S,masked", [(16, 1, False), (16, 1, True), (16, 3, False), (128, 3, True), (128, 16, False)])
+@pytest.mark.parametrize("where", ["query", "query rope", "committed", "prefix"])
+def test_nan_reaches_the_rows_that_see_it_and_no_others(b, bits, mode, H, S, masked, where):
+    p = Problem(H, S, 150, [140, 131, 64 + S, 400, 0, S], bits=bits, seed=22)
+    mask = torch.zeros(p.B, S, dtype=torch.int64) if masked else None       # (no row sees a draft)
+    clean, _ = p.reference(mask)
+    hit = torch.zeros(p.B * S, H, dtype=torch.bool)
+    if where.startswith("query"):
+        q = p.q_nope if where == "query" else p.q_pe
+        q[S, 3, 5] = float("nan")
+        q[2 * S, 15, 0] = float("inf")
+        hit[S, 3] = hit[2 * S, 15] = True
+    elif where == "committed":
+        slot = int(p.slot[1][20])
+        if bits == 8:
+            p.ckv_pages.view(-1, 512)[slot], p.exponents.view(-1)[slot] = 0, 255
+        else:
+            p.ckv_pages.view(-1, 512)[slot, 100] = float("nan")
+        hit[S:2 * S] = True
+    else:
+        p.ckv[77, 9] = float("nan")
+        hit[:] = True
+    got, lse, status = p.step(mask=mask, mode=MODES[mode])
+    assert status == 0
+    hit = hit.cuda()
+    assert torch.isnan(got[hit]).all() and torch.isnan(lse[hit]).all()
+    check(got[~hit][None], clean[~hit][None])
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_more_requests_than_are_ordered(b, bits):
+    """More than 4096 requests: no launch order, no descriptors."""
+    p = Problem(16, 2, 100, [2 + (i * 37) % 70 for i in range(4100)], bits=bits, seed=23)
+    got, lse, status = p.step()
+    assert status == 0
+    rows = [0, 1, 2, 3, 200, 201, 4098, 4099, 8190, 8191, 8198, 8199]
+    part = [r // 2 for r in rows[::2]]
+    q = Problem(16, 2, 100, [p.lens[r] for r in part], bits=bits, seed=23)
+    q.q_nope, q.q_pe, q.ckv, q.kpe, q.w_uk, q.w_uv = p.q_nope[rows], p.q_pe[rows], p.ckv, p.kpe, p.w_uk, p.w_uv
+    q.slot, q.ckv_pages, q.kpe_pages, q.exponents = [p.slot[r] for r in part], p.ckv_pages, p.kpe_pages, p.exponents
+    want, want_lse = q.reference()
+    check(got[rows], want, lse[rows], want_lse)
