@@ -21,11 +21,12 @@
  *   - Every pointer is a DEVICE pointer unless its comment says "host".
  *   - Tensors are bf16 (raw uint16 storage) unless stated; accumulation,
  *     softmax statistics, split partials and the combine are fp32.
- *   - q_pe and all cached rope keys arrive already rotated: no RoPE is applied.
+ *   - q_pe and all cached rope keys of a step arrive already rotated (typhoon_mla_rope_queries and
+ *     typhoon_mla_cache_append rotate them).
  *   - softmax_scale multiplies the sum of the nope and the rope logits; it must be
  *     positive and finite.
  *   - Log-sum-exps are natural logarithms of sum(exp(scaled logit)).
- *   - A single decode query attends to every cached token (no mask).
+ *   - A single decode query attends to every cached token (no mask; typhoon_mla_decode_draft has one).
  *   - Every call returns a status (0 = OK); nothing throws, aborts or traps.
  *     Work is enqueued on the given cudaStream_t (passed as void*) and the call
  *     returns without synchronising unless stated.
@@ -460,7 +461,7 @@ int typhoon_mla_cache_read(const typhoon_mla_cache_t* cache /* host */, const in
  * A row that sees nothing at all gets a zero output and lse = -inf.  What a row does not see does not reach it, whatever
  * it holds (NaN included); a row that sees a NaN becomes NaN (output and lse).  Rows j >= n are computed like the others.
  *   q_nope bf16 [B * S, H, 128], q_pe bf16 [B * S, H, 64], out bf16 [B * S, H, 128], lse_out optional fp32 [B * S, H]: row b * S + j
- *   block_table int32 [B, max_pages], seq_lens int32 [B]: per request (max_pages >= 1); bad page ids as in typhoon_mla_decode
+ *   block_table int32 [B, max_pages], seq_lens int32 [B]: per request (1 <= max_pages <= 2^23); bad page ids as in typhoon_mla_decode
  *   mode  AUTO, ABSORB or HYBRID (NAIVE: INVALID_ARG)
  *   workspace  typhoon_mla_draft_workspace_bytes, which also serves every step of fewer requests, fewer drafts or a narrower table
  * With an 8-bit cache the latent values are what the codes stand for; computation is as exact as over a 16-bit cache (values below

@@ -1272,7 +1272,7 @@ int typhoon_mla_combine_partials(const float* o_parts, const float* lse_parts, i
 }
 // ---- drafted tokens ---------------------------------------------------------------------------------
 static bool draft_sizes_valid(const typhoon_mla_shared_t* sh, int32_t B, int32_t S, int32_t max_pages, int32_t mode) {
-    return sh && B >= 1 && S >= 1 && S <= 64 && (int64_t)B * S <= TYPHOON_MLA_MAX_DRAFT_ROWS && max_pages >= 1 && max_pages <= (1 << 24) &&
+    return sh && B >= 1 && S >= 1 && S <= 64 && (int64_t)B * S <= TYPHOON_MLA_MAX_DRAFT_ROWS && max_pages >= 1 && max_pages <= (1 << 23) &&
            mode >= TYPHOON_MLA_MODE_AUTO && mode <= TYPHOON_MLA_MODE_HYBRID;
 }
 
