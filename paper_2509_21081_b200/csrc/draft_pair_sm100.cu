@@ -30,8 +30,17 @@
 // (Query absorption splits Q, from 32 bits; the split of P is here, from 32 bits as well.)
 //
 // Warp roles (12 warps per CTA): warp 0 loads K tiles (and Q), warp 2 the second operand; warp 1 allocates tensor memory and in
-// the even CTA issues both products; warp 3 lays out the tokens' powers of two; warps 4-11: softmax and epilogue, a thread per row and
-// 32 tokens of a tile.
+// the even CTA issues both products (in the odd one it requests W_UV into L2); warp 3 turns the tokens' exponent bytes into floats;
+// warps 4-11: softmax and epilogue, a thread per row and 32 tokens of a tile.
+//
+// What bounds it (B200; 64 requests of 1024 rows over 2112 tokens each, 16 / 8 bits: 236 / 281 us, 1.28 / 1.07 PFLOP/s; 74 requests of
+// 128 rows over 4096 tokens that nobody shares 74 / 82 us; 296 of 128 rows over 512 tokens 61 / 66; one tile per pair 12.8 / 14.0):
+//   - 16 bits: a tile takes 2480 clocks, 2176 of them products; the rest is the reload of V, for which there is one stage (K, V, Q and P
+//     fill shared memory; 136 KB come from L2 per CTA and tile).
+//   - 8 bits: 3100 clocks for 2100 of products: the softmax warps' own chain (two per scheduler, in step by the vote).  Sixteen of them
+//     with half the tokens each take as long; requesting the next logits earlier needs more registers than there are.
+//   - an item costs 7000 clocks beside its tiles: result 3000, last product 1100, drafts' values read through 1000, first logits 1000.
+//     Hence pairs that walk through items with loads one item ahead (one item per pair and launch: 10 us each).
 #include <algorithm>
 #include <cstddef>
 
