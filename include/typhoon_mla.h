@@ -429,7 +429,7 @@ int typhoon_mla_rope_queries(const typhoon_mla_rope_t* rope /* host */, const vo
  * stride ld_kpe; strides in elements, multiples of 8), rotated to positions[t] first unless rope and positions are both NULL,
  * go to slot slots[t] = page * page_size + slot in page.  Negative slots are skipped (padding tokens); a slot at or past
  * num_pages * page_size is not dereferenced and sets TYPHOON_MLA_STATUS_BAD_PAGE in *status (device word, may be NULL; it is
- * only ORed into).  Slots of one call that are not negative differ from one another.
+ * only ORed into).  Slots of one call that are not negative differ from one another, and the rows read are not among them.
  * With an 8-bit cache the row is encoded as it is written: the exponent is the smallest one for which the row's largest magnitude
  * fits 448 (at least -126, byte 1), the codes are the row divided by that power of two, rounded to nearest even (and never to
  * 2^128, which bf16 does not hold: 1.875 * 2^127 then); a row with an infinity or a NaN gets byte 255 and codes of zero.

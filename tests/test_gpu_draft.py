@@ -1,4 +1,6 @@
 """Decode attention for drafted tokens (chains, trees, any mask) over 16- and 8-bit caches, against the definition in 64 bits."""
+import random
+
 import pytest
 import torch
 
@@ -407,3 +409,68 @@ def test_more_requests_than_are_ordered(b, bits):
     q.slot, q.ckv_pages, q.kpe_pages, q.exponents = [p.slot[r] for r in part], p.ckv_pages, p.kpe_pages, p.exponents
     want, want_lse = q.reference()
     check(got[rows], want, lse[rows], want_lse)
+
+
+@pytest.mark.parametrize("seed", range(32))
+def test_drawn_steps(b, seed):
+    """Sizes, masks, counts, modes and library settings at random; half of the steps are captured and replayed."""
+    g = random.Random(seed)
+    H, S, B = g.choice([16, 32, 48, 64, 80, 112, 128]), g.choice([1, 1, 2, 3, 5, 8, 13, 33, 64]), g.randint(1, 9)
+    if H * S > 2048:
+        H = 16
+    Ls = g.choice([0, 1, 63, 129, 500, 1500])
+    lens = [max(0, g.choice([S, S + 1, g.randint(0, 130), g.randint(100, 900)])) for _ in range(B)]
+    bits = g.choice([8, 16])
+    p = Problem(H, S, Ls, lens, bits=bits, page=g.choice([64, 128]), seed=100 + seed)
+    kind = g.choice(["chain", "tree", "any"])
+    mask = None if kind == "chain" else random_tree(S, B, seed) if kind == "tree" else \
+        torch.tensor([[g.getrandbits(64) - (1 << 63) for _ in range(S)] for _ in range(B)], dtype=torch.int64)
+    counts = None if g.random() < 0.5 else [g.randint(-1, S + 1) for _ in range(B)]
+    mode = g.choice([0, 1, 2])
+    want, want_lse = p.reference(mask, counts)
+    b.typhoon_mla_set_overlap(g.random() < 0.7)
+    b.typhoon_mla_set_programmatic_launch(g.random() < 0.7)
+    b.typhoon_mla_set_stacked_absorb(g.random() < 0.7)
+    b.typhoon_mla_set_naive_schedule(g.choice([0, 1, 2]))
+    try:
+        dec = p.decoder()
+        got, lse, status = p.step(dec, mask, counts, mode)
+        assert status == 0
+        check(got, want, lse, want_lse)
+        if seed % 2:
+            a = [x.cuda() for x in (p.q_nope, p.q_pe, p.table, torch.tensor(p.lens, dtype=torch.int32))]
+            kw = dict(tree_mask=None if mask is None else mask.cuda(),
+                      draft_lens=None if counts is None else torch.tensor(counts, dtype=torch.int32, device="cuda"), mode=mode)
+            cache, out = p.cache(), torch.empty_like(a[0])
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                dec.decode_draft(a[0], a[1], cache, a[2], a[3], out=out, **kw)
+            for _ in range(3):
+                out.zero_()
+                graph.replay()
+                assert torch.equal(out.double(), got)
+    finally:
+        b.typhoon_mla_set_overlap(True)
+        b.typhoon_mla_set_programmatic_launch(True)
+        b.typhoon_mla_set_stacked_absorb(True)
+        b.typhoon_mla_set_naive_schedule(0)
+
+
+def test_steps_at_once(b):
+    """Four decoders on four streams, both caches and both modes, many steps in flight: each gives what it gives alone."""
+    runs = []
+    for i, (bits, mode) in enumerate([(16, 1), (8, 1), (16, 2), (8, 2)]):
+        p = Problem(32, 5, 700, [5 + 97 * k % 600 for k in range(20)], bits=bits, seed=30 + i)
+        a = [x.cuda() for x in (p.q_nope, p.q_pe)] + [p.cache(), p.table.cuda(), torch.tensor(p.lens, dtype=torch.int32, device="cuda")]
+        dec, s = p.decoder(), torch.cuda.Stream()
+        runs.append((dec, a, mode, s, dec.decode_draft(*a, mode=mode)))
+    torch.cuda.synchronize()
+    got = [[] for _ in runs]
+    for _ in range(25):
+        for k, (dec, a, mode, s, _) in enumerate(runs):
+            with torch.cuda.stream(s):
+                got[k].append(dec.decode_draft(*a, mode=mode))
+    torch.cuda.synchronize()
+    for k, (dec, _, _, _, want) in enumerate(runs):
+        assert all(torch.equal(x, want) for x in got[k])
+        assert b.typhoon_mla_check_status(dec.shared, raise_on_error=False) == 0
