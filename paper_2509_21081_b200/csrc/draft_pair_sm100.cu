@@ -199,7 +199,6 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
     cluster_sync();
     tc_fence_after();
     const uint32_t tmem_base = __shfl_sync(0xffffffffu, sh->tmem_base, 0);
-    pdl_wait();
 
     // Work items: over the prefix (absorb-only steps of a 16-bit cache), chunk fastest, then 128 rows; over the suffixes, row tile
     // fastest (they share the tokens), then chunk, then request in longest-first order.  A pair takes every
@@ -261,6 +260,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
         return it;
     };
     const int n_rounds = n_items > 0 ? (n_items + n_pairs - 1) / n_pairs : 0;
+    pdl_wait();
 
     bool bad_page = false;   // loading warps only: a page id of the caller's table was out of range
     auto page_at = [&](const Item& it, int t0) {   // physical page of token t0 < tok_end
@@ -313,8 +313,9 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
         };
         bool ok = true;
         int g = 0, n = 0;
+        Item it = pf;
         for (int k = 0; k < n_rounds && ok; ++k) {
-            const Item it = item_at(k, desc_of(k));
+            if (k > 0) it = item_at(k, desc_of(k));
             const CUtensorMap* tc = it.b < 0 ? &tm_ckv_sh : &tm_ckv;
             for (int j = 0; j < it.n_tiles && ok; ++j, ++g) {
                 int page, slot;
