@@ -657,10 +657,8 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                         // (a row without a reference: any logit exceeds it)
                         exceed = top > (m_ref == -INFINITY ? -INFINITY : kRescale16);
                     }
-                    // probabilities against the current reference: final unless the CTA votes for a rescale (an item's first tile has no
-                    // reference yet, and does not vote)
-                    if (j > 0) probabilities();
                 }
+                // (an item's first tile has no reference yet, and does not vote)
                 if (j == 0 || vote_or<SM>(exceed)) {
                     // the row's largest logit (8 bits: times the token's power of two)
                     if (E8 && ok) {
@@ -715,9 +713,9 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
 #pragma unroll
                             for (int c = 0; c < TPT; ++c) x[c] += d;
                         }
-                        probabilities();
                     }
                 }
+                if (ok) probabilities();
                 if (E8 && ok) {
                     l_part[0] += tsum;
                     if (j < it.n_tiles - 1) load_sigma(g + 1);
