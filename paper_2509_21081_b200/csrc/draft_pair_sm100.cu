@@ -523,16 +523,14 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
             const int64_t row0 = it.row0;
             if (it.n_tiles == 0) {
                 // empty chunk: weight zero in the merge (a request without any latent token: zero latent output)
-                const int r = 64 * (int)rank + (int)threadIdx.x - 128;
-                if (threadIdx.x < 192 && r < n_rows) {
-                    if (direct) {
-                        p.lse_direct[row0 + r] = -INFINITY;
-                        for (int l = 0; l < 512; l += 8)
-                            *reinterpret_cast<uint4*>(p.o_lat_direct + (row0 + r) * 512 + l) = make_uint4(0, 0, 0, 0);
-                    } else {
-                        p.lse_part[(int64_t)it.slot * all_rows + row0 + r] = -INFINITY;
-                    }
+                const int tid = (int)threadIdx.x - 128, own = min(max(n_rows - 64 * (int)rank, 0), 64);
+                const int64_t r0 = row0 + 64 * (int)rank;
+                if (tid < own) {
+                    if (direct) p.lse_direct[r0 + tid] = -INFINITY;
+                    else p.lse_part[(int64_t)it.slot * all_rows + r0 + tid] = -INFINITY;
                 }
+                if (direct)
+                    for (int i = tid; i < own * 64; i += SM) reinterpret_cast<uint4*>(p.o_lat_direct + r0 * 512)[i] = make_uint4(0, 0, 0, 0);
                 continue;
             }
             const bool mine = 64 * (int)rank + row < n_rows;      // (else nobody's: sees nothing)
