@@ -24,7 +24,7 @@ def stored(latent, bits):
     for r in x:
         s = F.pow2_scale(abs(r).max())
         rows.append(F.e4m3_decode_table()[F.e4m3_encode(r / s)] * s)
-    return torch.tensor(rows, dtype=torch.float64)
+    return torch.stack([torch.as_tensor(r, dtype=torch.float64) for r in rows])
 
 
 @pytest.mark.parametrize("bits", [16, 8])
