@@ -474,3 +474,28 @@ def test_steps_at_once(b):
     for k, (dec, _, _, _, want) in enumerate(runs):
         assert all(torch.equal(x, want) for x in got[k])
         assert b.typhoon_mla_check_status(dec.shared, raise_on_error=False) == 0
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_offsets_past_32_bits(b, bits):
+    """A cache of more than 2^32 bytes whose last pages are used: written, read back and attended there."""
+    p = Problem(16, 3, 100, [200, 3, 130], bits=bits, seed=24, poison=False)
+    n = p.kpe_pages.shape[0]
+    pages = (2 ** 32) // (64 * (1024 if bits == 16 else 512)) + 1000
+    first = pages - n
+    big = b.PagedCache(torch.zeros(pages, 64, 512, dtype=torch.bfloat16 if bits == 16 else torch.uint8, device="cuda"),
+                       torch.zeros(pages, 64, 64, dtype=torch.bfloat16, device="cuda"),
+                       None if bits == 16 else torch.zeros(pages, 64, dtype=torch.uint8, device="cuda"))
+    small = p.cache()
+    slots = torch.cat(p.slot).cuda()
+    ckv, kpe = b.typhoon_mla_cache_read(small, slots)
+    b.typhoon_mla_cache_append(big, ckv, kpe, slots + first * 64)
+    again, keys = b.typhoon_mla_cache_read(big, slots + first * 64)
+    assert torch.equal(again, ckv) and torch.equal(keys, kpe)
+    assert not big.kpe_pages[:first].any()
+    want, want_lse = p.reference()
+    p.cache, p.table = lambda: big, torch.where(p.table >= 0, p.table + first, p.table)
+    for mode in (1, 2):
+        got, lse, status = p.step(mode=mode)
+        assert status == 0
+        check(got, want, lse, want_lse)
