@@ -54,7 +54,7 @@ using namespace sm100;
 
 constexpr int TOK = 128;
 constexpr int SLAB = 64 * 128;                   // [64 rows][128 bytes], swizzled
-constexpr float kLog2Off = 4.f, kLog2Room = 4.f; // 8 bits: P at the reference is 2^4, and at most 2^4 times that
+constexpr float kLog2Off = 4.f, kMostP = 256.f;  // 8 bits: P at the reference is 2^4, and at most 2^8
 constexpr float kLog2Floor = 100.f;              // 8 bits: references are no further below the largest weight than this
 constexpr float kRescale16 = 8.f;                // 16 bits: log2 above the reference
 
@@ -643,12 +643,12 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                         // some 2^x sigma kappa above its limit?  First by the largest of both factors.  (And kappa, with or without a
                         // power of two, stays far from what 32 bits hold.)
                         const float most_k = max_of(sigma) * kappa;
-                        exceed = m_ref == -INFINITY ? top != -INFINITY : fast_exp2(top) * most_k > 256.f;     // 2^(kLog2Off + kLog2Room)
+                        exceed = m_ref == -INFINITY ? top != -INFINITY : fast_exp2(top) * most_k > kMostP;
                         if (exceed && m_ref != -INFINITY) {
                             float most = 0.f;
 #pragma unroll
                             for (int c = 0; c < TPT; ++c) most = fmaxf(most, fast_exp2(x[c]) * (sigma[E8 ? c : 0] * kappa));
-                            exceed = most > 256.f;
+                            exceed = most > kMostP;
                         }
                         exceed |= fmaxf(most_k, kappa) > 0x1p105f;
                     } else {
