@@ -464,8 +464,10 @@ int typhoon_mla_cache_read(const typhoon_mla_cache_t* cache /* host */, const in
  *   block_table int32 [B, max_pages], seq_lens int32 [B]: per request (1 <= max_pages <= 2^23); bad page ids as in typhoon_mla_decode
  *   mode  AUTO, ABSORB or HYBRID (NAIVE: INVALID_ARG)
  *   workspace  typhoon_mla_draft_workspace_bytes, which also serves every step of fewer requests, fewer drafts or a narrower table
- * With an 8-bit cache the latent values are what the codes stand for; computation is as exact as over a 16-bit cache (values below
- * 2^-90 of magnitude count as zeros in the output).
+ * With an 8-bit cache the latent values are what the codes stand for; computation is as exact as over a 16-bit cache: a token's weight is
+ * good to 2^-8 of itself, as in bf16, down to 2^-19 of the row's largest contribution (weight times the token's power of two), and to
+ * 2^-27 of that below; an element of the absorbed query to 2^-8 of itself down to 2^-10 of the row's largest, and to 2^-18 of that
+ * below (values below 2^-90 of magnitude count as zeros in the output).
  * B * S <= TYPHOON_MLA_MAX_DRAFT_ROWS; tcgen05 kernel path only (UNSUPPORTED_DIMS otherwise); streams, capture and errors as
  * typhoon_mla_decode.
  */

@@ -14,20 +14,26 @@
 // sees nothing in a chunk gets weight zero there.
 //
 // 8-bit latent rows.  Widening codes to 16 bits on the way would take as much shared-memory traffic as the products themselves.
-// Instead the products run on the codes (kind::f8f6f4, twice the rate of 16 bits) and the other operand is split into two E4M3
-// numbers, the nearest one and the nearest one to the rest: 4 significant bits, a sign and 4 more, at least the 8 bits of bf16 (with
-// m = the mantissa of a bf16 value as an integer in [128, 256) the nearest multiple of 16 and the rest, at most 8, are both exact;
-// split from 32 bits the sum is off by 6e-4 of the value in the mean square, bf16 by 1.6e-3).  Two products at twice the rate: the
-// time and the operand bytes of the 16-bit kernel, on half the cache bytes.  What is left of the range: a row of Q is scaled by a
-// power of two to an amax in [224, 448], so an element loses bits only where it is 2^-10 of the row's largest (by 2^-18 of that at
-// most); P is held to at most 2^8 with 2^4 at the reference, so a weight is good to 2^-14 of the row's largest contribution.
+// Instead the products run on the codes (kind::f8f6f4, twice the rate of 16 bits) and the other operand is split into 8-bit numbers.
+//   Q: two E4M3 numbers, the nearest one and the nearest one to the rest: 4 significant bits, a sign and 4 more, at least the 8 bits of
+//   bf16 (with m = the mantissa of a bf16 value as an integer in [128, 256) the nearest multiple of 16 and the rest, at most 8, are
+//   both exact; split from 32 bits the sum is off by 6e-4 of the value in the mean square, bf16 by 1.6e-3).  A row is scaled by a
+//   power of two to an amax in [224, 448], so an element loses bits only where it is 2^-10 of the row's largest (by 2^-18 of that at
+//   most, in each of 512 dims).
+//   P: three E5M2 numbers of 3 significant bits.  A weight may be small and still count, being one of many: what its rounding takes away
+//   has to be small next to the weight itself, as with bf16, not next to the row's largest.  (Two E4M3 numbers end at 2^-9, 2^-14 of the
+//   reference: 4096 equal tokens behind one with 0.8 of the weight vanished, 16 % of the output.)  With 2^11 at the reference and at most
+//   2^15 a weight is good to 2^-8.6 of itself (5e-4 in the mean square) down to 2^-19 of the row's largest contribution, below that to
+//   2^-27.8 of it: 2^19 tokens in an item could lose 2^-8.8 together.  Two E5M2 numbers would have 7 bits.
+// Two and three products at twice the rate, on half the cache bytes.
 // The rope part (16-bit, unscaled) goes to an accumulator of its own, and a logit is S_lat * 2^(tau + e_t) + S_rope.  The token's power
 // of two belongs to its values as well: with x the scaled logit in log2 units P = 2^(x + e_t - n) against a reference n of the x + e_t,
 // while the row sum is of 2^(x - m) against a reference m of the x (per thread; any within 2^40 will do in 32 bits):
-// P = 2^(x - m) * 2^e_t * kappa with kappa = 2^(m - n) per thread and tile.  n is kept within 2^100 of the largest weight (and of the
-// largest power of two), where kappa is a normal number: tokens whose values are under 2^-100 next to their weight count as zeros.
+// P = 2^(x - m) * 2^e_t * kappa with kappa = 2^(m - n) per thread and tile.  n is kept within 2^92 of the largest weight (and of the
+// largest power of two), where kappa is a normal number: tokens whose values are under 2^-92 next to their weight count as zeros.
 //
-// (Query absorption splits Q, from 32 bits; the split of P is here, from 32 bits as well.)
+// (Query absorption splits Q, from 32 bits.  P is split here, from its rounding to fp16, 11 bits: the high byte of an fp16 number is an
+// E5M2 number, so a term is a byte selection and the rest an exact subtraction.)
 //
 // Warp roles (12 warps per CTA): warp 0 loads K tiles (and Q), warp 2 the second operand; warp 1 allocates tensor memory and in
 // the even CTA issues both products (in the odd one it requests W_UV into L2); warp 3 turns the tokens' exponent bytes into floats;
@@ -37,7 +43,7 @@
 // 128 rows over 4096 tokens that nobody shares 74 / 82 us; 296 of 128 rows over 512 tokens 61 / 66; one tile per pair 12.8 / 14.0):
 //   - 16 bits: a tile takes 2480 clocks, 2176 of them products; the rest is the reload of V, for which there is one stage (K, V, Q and P
 //     fill shared memory; 136 KB come from L2 per CTA and tile).
-//   - 8 bits: 3100 clocks for 2100 of products: the softmax warps' own chain (two per scheduler, in step by the vote).  Sixteen of them
+//   - 8 bits: 3600 clocks for 2600 of products (two terms of P: 3100 for 2100): the softmax warps' own chain (two per scheduler, in step by the vote).  Sixteen of them
 //     with half the tokens each take as long; requesting the next logits earlier needs more registers than there are.
 //   - an item costs 7000 clocks beside its tiles: result 3000, last product 1100, drafts' values read through 1000, first logits 1000.
 //     Hence pairs that walk through items with loads one item ahead (one item per pair and launch: 10 us each).
@@ -54,8 +60,8 @@ using namespace sm100;
 
 constexpr int TOK = 128;
 constexpr int SLAB = 64 * 128;                   // [64 rows][128 bytes], swizzled
-constexpr float kLog2Off = 4.f, kMostP = 256.f;  // 8 bits: P at the reference is 2^4, and at most 2^8
-constexpr float kLog2Floor = 100.f;              // 8 bits: references are no further below the largest weight than this
+constexpr float kLog2Off = 11.f, kMostP = 32768.f;  // 8 bits: P at the reference is 2^11, and at most 2^15 (fp16 and E5M2 end above that)
+constexpr float kLog2Floor = 92.f;               // 8 bits: references are no further below the largest weight than this
 constexpr float kRescale16 = 8.f;                // 16 bits: log2 above the reference
 
 struct DraftParams {
@@ -90,7 +96,7 @@ struct Shape {
     static constexpr int NV = E8 ? 1 : 2;                     // copy groups of the second operand
     static constexpr int V_BYTES = (E8 ? 4 : 8) * SLAB;       // a stage: 128 tokens x 256 dims
     static constexpr int Q_BYTES = 9 * SLAB;                  // 8 bits: both terms of 4 slabs, and rope
-    static constexpr int P_BYTES = 2 * SLAB;                  // 16 bits: [2 token halves][64 rows][64]; 8 bits: [2 terms][64 rows][128]
+    static constexpr int P_BYTES = (E8 ? 3 : 2) * SLAB;       // 16 bits: [2 token halves][64 rows][64]; 8 bits: [3 terms][64 rows][128]
     static constexpr int GROUP = E8 ? 32 : 16;                // tokens of one MMA of the second product
     static constexpr int TPT = 32;                            // tokens of a tile per softmax thread
     static constexpr int PARTS = TOK / TPT;                   // softmax threads per row
@@ -157,6 +163,21 @@ __device__ __forceinline__ float max_of(const float (&x)[N]) {
         b = max3(b, x[N / 2 + c], x[N / 2 + c + 1]);
     }
     return fmaxf(max3(a, b, x[N / 2 - 1]), x[N - 1]);
+}
+
+// 4 values as fp16 (two words, the lower half first): codes of three E5M2 terms, the value cut to 3 significant bits, the rest cut to 3, and the
+// rest of that rounded to 3 (half up: its bits are a magnitude).  Not a number: the first term is not.
+__device__ __forceinline__ void split4_e5m2(uint32_t a, uint32_t b, uint32_t& first, uint32_t& second, uint32_t& third) {
+    auto cut_off = [](uint32_t x) {
+        uint32_t d;
+        asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(d) : "r"(x), "r"(x & 0xff00ff00u));
+        return d;
+    };
+    auto high_bytes = [](uint32_t x, uint32_t y) { return __byte_perm(x, y, 0x7531); };
+    const uint32_t a1 = cut_off(a), b1 = cut_off(b);
+    first = high_bytes(a, b);
+    second = high_bytes(a1, b1);
+    third = high_bytes(cut_off(a1) + 0x00800080u, cut_off(b1) + 0x00800080u);
 }
 
 template <bool E8>
@@ -391,7 +412,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
         // ---------------- both products (even CTA)
         constexpr uint32_t idesc_s = idesc_bf16(128, 128, false, false);
         constexpr uint32_t idesc_s8 = idesc_e4m3(128, 128, false, false);
-        constexpr uint32_t idesc_o = E8 ? idesc_e4m3(128, 256, false, true) : idesc_bf16(128, 256, false, true);
+        constexpr uint32_t idesc_o = E8 ? idesc_e5m2_e4m3(128, 256, false, true) : idesc_bf16(128, 256, false, true);
         const uint32_t qa = smem_u32(sQ), va = smem_u32(sV), pa = smem_u32(sP);
         bool ok = true;
         int g = 0, n = 0;
@@ -421,7 +442,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                                         const uint64_t da = smem_desc_k_sw128(qa + (4 * t + sl) * SLAB);
                                         const uint64_t db = smem_desc_k_sw128(ka + (sl - HALF * h) * SLAB);
 #pragma unroll
-                                        for (int i = 0; i < 4; ++i) umma_pair_e4m3(d, da + 2 * i, db + 2 * i, idesc_s8, (sl | t | i) != 0);
+                                        for (int i = 0; i < 4; ++i) umma_pair_8bit(d, da + 2 * i, db + 2 * i, idesc_s8, (sl | t | i) != 0);
                                     }
                                 if (h == 1) {
                                     const uint64_t da = smem_desc_k_sw128(qa + 8 * SLAB), db = smem_desc_k_sw128(ka + HALF * SLAB);
@@ -470,8 +491,9 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                                 const uint64_t db0 = smem_desc_mn_sw128(va + st * X::V_BYTES + nb * SLAB, SLAB, 1024);
                                 auto product = [&](int i) {
                                     const uint64_t db = db0 + (i >> 1) * (2 * SLAB / 16) + (i & 1) * 256;
-                                    umma_pair_e4m3(d, da0 + 2 * i, db, idesc_o, (t | i) != 0);
-                                    umma_pair_e4m3(d, da0 + SLAB / 16 + 2 * i, db, idesc_o, 1);
+                                    umma_pair_8bit(d, da0 + 2 * i, db, idesc_o, (t | i) != 0);
+                                    umma_pair_8bit(d, da0 + SLAB / 16 + 2 * i, db, idesc_o, 1);
+                                    umma_pair_8bit(d, da0 + 2 * SLAB / 16 + 2 * i, db, idesc_o, 1);
                                 };
                                 if (n_k == 4) {
 #pragma unroll
@@ -572,7 +594,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                 }
                 // x[c]: the logit in log2 units above a reference: 16 bits, the row's; 8 bits, this thread's (its row sum's)
                 float x[TPT], kappa = 0.f, top = -INFINITY, tsum = 0.f;
-                uint32_t pk[TPT / 2];                  // 16 bits: pairs; 8 bits: words of the first term, then of the second
+                uint32_t pk[TPT / 2];                  // pairs, 16 bits: bf16; 8 bits: fp16
                 const float base = E8 ? (m_sum == -INFINITY ? 0.f : m_sum) : (m_ref == -INFINITY ? 0.f : m_ref);
                 bool exceed = false;
                 // P in the form of the product's operand: 16 bits, 2^x; 8 bits, 2^x sigma kappa, and the sum of 2^x
@@ -585,9 +607,8 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                         if (E8) {
                             const uint64_t pa = pack_f32x2(p0, p1), pb = pack_f32x2(p2, p3);
                             sum = add_f32x2(add_f32x2(pa, pb), sum);
-                            split4_x2(mul_f32x2(pa, mul_f32x2(pack_f32x2(sigma[E8 ? c : 0], sigma[E8 ? c + 1 : 0]), kappa2)),
-                                      mul_f32x2(pb, mul_f32x2(pack_f32x2(sigma[E8 ? c + 2 : 0], sigma[E8 ? c + 3 : 0]), kappa2)), pk[c / 4],
-                                      pk[TPT / 4 + c / 4]);
+                            pk[c / 2] = pack_f16_x2(mul_f32x2(pa, mul_f32x2(pack_f32x2(sigma[E8 ? c : 0], sigma[E8 ? c + 1 : 0]), kappa2)));
+                            pk[c / 2 + 1] = pack_f16_x2(mul_f32x2(pb, mul_f32x2(pack_f32x2(sigma[E8 ? c + 2 : 0], sigma[E8 ? c + 3 : 0]), kappa2)));
                         } else {
                             pk[c / 2] = pack_bf16(p0, p1);
                             pk[c / 2 + 1] = pack_bf16(p2, p3);
@@ -730,13 +751,15 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                     // P, once the previous tile's product has read its buffer (the previous item's last: awaited in its epilogue)
                     if (j > 0) mbar_wait(&sh->o_done[(g - 1) & 1], ((g - 1) >> 1) & 1, abort_flag);
                     if (E8) {
-                        // row of 128 tokens, one byte each, in both terms
+                        // row of 128 tokens, one byte each, in all three terms
 #pragma unroll
                         for (int c = 0; c < TPT / 16; ++c) {
                             uint8_t* at = sP + row * 128 + (((part * (TPT / 16) + c) ^ (row & 7)) * 16);
-                            *reinterpret_cast<uint4*>(at) = make_uint4(pk[4 * c], pk[4 * c + 1], pk[4 * c + 2], pk[4 * c + 3]);
-                            *reinterpret_cast<uint4*>(at + SLAB) =
-                                make_uint4(pk[TPT / 4 + 4 * c], pk[TPT / 4 + 4 * c + 1], pk[TPT / 4 + 4 * c + 2], pk[TPT / 4 + 4 * c + 3]);
+                            uint32_t t[3][4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) split4_e5m2(pk[8 * c + 2 * i], pk[8 * c + 2 * i + 1], t[0][i], t[1][i], t[2][i]);
+#pragma unroll
+                            for (int i = 0; i < 3; ++i) *reinterpret_cast<uint4*>(at + i * SLAB) = make_uint4(t[i][0], t[i][1], t[i][2], t[i][3]);
                         }
                     } else {
                         uint8_t* p_row = sP + half * SLAB + row * 128;
@@ -803,7 +826,7 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                 for (int i = 0; i < PARTS; ++i) l += sh->red[i][row];
             }
             // l = 0: nothing visible in this chunk.  l = NaN: some logit is not finite, and the row becomes NaN.
-            const float inv = l == 0.f ? 0.f : (E8 ? fast_exp2(m_ref - kLog2Off - m) : 1.f) / l;
+            const float inv = l == 0.f ? 0.f : (E8 ? fast_exp2((m_ref - m) - kLog2Off) : 1.f) / l;
             if (part == 0 && mine) {
                 const float lse = l == 0.f ? -INFINITY : l == l ? (m + log2f(l)) * kLn2 : kLseNotFinite;
                 const int64_t r = row0 + 64 * (int)rank + row;

@@ -229,6 +229,10 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, bool a_mn_major,
 __host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N, bool a_mn_major, bool b_mn_major) {
     return idesc_bf16(M, N, a_mn_major, b_mn_major) & ~((7u << 7) | (7u << 10));
 }
+// E5M2 x E4M3 -> fp32 (kind::f8f6f4; format code 1 in A's field, 0 in B's).
+__host__ __device__ constexpr uint32_t idesc_e5m2_e4m3(int M, int N, bool a_mn_major, bool b_mn_major) {
+    return idesc_e4m3(M, N, a_mn_major, b_mn_major) | (1u << 7);
+}
 
 // The same with both operands in IEEE half precision (format code 0 in both operand fields).
 __host__ __device__ constexpr uint32_t idesc_f16(int M, int N, bool a_mn_major, bool b_mn_major) {
@@ -368,7 +372,7 @@ __device__ __forceinline__ void umma_pair_ts(uint32_t d_tmem, uint32_t a_tmem, u
         : "memory");
 }
 // The same on 8-bit operands, 32 values deep.
-__device__ __forceinline__ void umma_pair_e4m3(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void umma_pair_8bit(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
         "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc),
@@ -494,21 +498,13 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return d;
 }
 
-// split4 of two packed pairs of non-negative values.  The first term is the value rounded to 4 significant bits by Dekker's splitting (with
-// 2^20 + 1), which is the nearest E4M3 number where that is a normal one and within half a step of the smallest below; the codes then
-// convert without a way back from the first.
-__device__ __forceinline__ void split4_x2(uint64_t ab, uint64_t cd, uint32_t& first, uint32_t& second) {
-    const uint64_t k = pack_f32x2(1048577.f, 1048577.f), minus = pack_f32x2(-1.f, -1.f);
-    const uint64_t u = mul_f32x2(ab, k), v = mul_f32x2(cd, k);
-    const uint64_t hu = fma_f32x2(fma_f32x2(ab, minus, u), minus, u), hv = fma_f32x2(fma_f32x2(cd, minus, v), minus, v);
-    const uint64_t lu = fma_f32x2(hu, minus, ab), lv = fma_f32x2(hv, minus, cd);
-    float a, b, c, d;
-    unpack_f32x2(hu, a, b);
-    unpack_f32x2(hv, c, d);
-    first = e4m3_pair(a, b) | (e4m3_pair(c, d) << 16);
-    unpack_f32x2(lu, a, b);
-    unpack_f32x2(lv, c, d);
-    second = e4m3_pair(a, b) | (e4m3_pair(c, d) << 16);
+// Two fp32 lanes as fp16, the lower half first; beyond its range its largest number.
+__device__ __forceinline__ uint32_t pack_f16_x2(uint64_t ab) {
+    float a, b;
+    unpack_f32x2(ab, a, b);
+    uint32_t d;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;\n" : "=r"(d) : "f"(b), "f"(a));
+    return d;
 }
 
 // ---------------------------------------------------------------- TMEM <-> registers
