@@ -238,7 +238,8 @@ int typhoon_mla_decode(const typhoon_mla_shared_t* shared,
  * over n_parts partials, o_parts fp32 [n_parts, B, H, 128] and lse_parts fp32
  * [n_parts, B, H] (device, 16-byte aligned) -> out bf16 [B, H, 128] and the
  * optional lse_out fp32 [B, H].  Rows whose partials are all empty give zeros
- * and -inf.  Head sharding needs no call of its own: a device prepares and
+ * and -inf; a row with an LSE that is a NaN or +inf becomes NaN (both outputs),
+ * whatever values stand beside it.  Head sharding needs no call of its own: a device prepares and
  * decodes H / G heads (weights and queries sliced by head) and the bf16
  * outputs are gathered along the head axis.
  * Errors: as typhoon_mla_decode; INVALID_ARG for a null lse_partial or

@@ -291,7 +291,8 @@ __global__ void __launch_bounds__(256) combine_kernel(const float* __restrict__ 
             acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
             z += w;
         }
-        float inv = 1.f / z;
+        // (a caller's partial may have finite values beside an LSE that is no number: its weight is unknown, so the row is)
+        float inv = m < kLseNotFinite ? 1.f / z : __int_as_float(0x7fc00000);
         acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
     }
     if (out_fp32) {
