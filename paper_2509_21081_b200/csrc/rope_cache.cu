@@ -399,8 +399,9 @@ int typhoon_mla_cache_append(const typhoon_mla_cache_t* cache, const void* ckv, 
                              const typhoon_mla_rope_t* rope, const int32_t* positions, const int64_t* slots, int64_t T, int32_t* status,
                              void* stream) {
     api_set_last_launches(0);
-    if (!cache_valid(cache) || T < 0 || (rope == nullptr) != (positions == nullptr) || (rope && !rope_valid(rope))) return TYPHOON_MLA_ERR_INVALID_ARG;
-    if (T == 0) return TYPHOON_MLA_OK;
+    if (!cache_valid(cache) || T < 0 || (rope && !rope_valid(rope))) return TYPHOON_MLA_ERR_INVALID_ARG;
+    if (T == 0) return TYPHOON_MLA_OK;      // (no tokens: an empty array of positions may have no address)
+    if ((rope == nullptr) != (positions == nullptr)) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (!ckv || !kpe || !slots || !aligned(ckv, 16) || !aligned(kpe, 16) || !aligned(positions, 4) || !aligned(slots, 8) || !aligned(status, 4))
         return TYPHOON_MLA_ERR_INVALID_ARG;
     if (ld_ckv < 512 || ld_ckv % 8 || ld_kpe < 64 || ld_kpe % 8) return TYPHOON_MLA_ERR_INVALID_ARG;
