@@ -30,9 +30,13 @@ class TyphoonMLADecoder:
         self.shared = prepare(self.dims, ckv_shared, kpe_shared, self.w_uk, self.w_uv)
         nbytes = _b.typhoon_mla_workspace_bytes(self.shared, self.max_batch, self.max_pages, self.page_size)
         self.max_drafts = int(max_drafts)
-        if self.max_drafts > 0:
-            nbytes = max(nbytes, _b.typhoon_mla_draft_workspace_bytes(self.shared, self.max_batch, self.max_drafts, self.max_pages,
-                                                                      self.page_size))
+        if self.max_drafts != 0:
+            dbytes = _b.typhoon_mla_draft_workspace_bytes(self.shared, self.max_batch, self.max_drafts, self.max_pages, self.page_size)
+            if dbytes == 0:
+                self.shared.free()
+                raise ValueError(f"no steps of {self.max_drafts} drafts for {self.max_batch} requests over tables of {self.max_pages} pages: "
+                                 "1 to 64 drafts, at most 2^20 rows, at least one page of 64 or 128 tokens")
+            nbytes = max(nbytes, dbytes)
         self.workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device="cuda")
         sbytes = _b.typhoon_mla_host_staging_bytes(self.shared, self.max_batch, self.max_pages)
         self.staging = torch.empty(max(sbytes, 256), dtype=torch.uint8, device="cuda")

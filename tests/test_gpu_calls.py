@@ -18,3 +18,19 @@ def test_no_tokens():
     b.typhoon_mla_rope_queries(rope, q[..., 128:], pos, torch.empty(0, 16, 64, dtype=bf, device="cuda"), q[..., :128],
                                torch.empty(0, 16, 128, dtype=bf, device="cuda"))
     assert not cache.ckv_pages.any() and not cache.kpe_pages.any()
+
+
+@pytest.mark.parametrize("sizes", [dict(max_drafts=65), dict(max_drafts=-1), dict(max_batch=1 << 15, max_drafts=33), dict(max_pages=0, max_drafts=2),
+                                   dict(max_pages=(1 << 23) + 1, max_drafts=2)])
+def test_decoder_of_steps_that_are_refused(sizes):
+    """Refused where it is built, not at the first step that does not fit."""
+    from paper_2509_21081_b200.decoder import TyphoonMLADecoder
+    bf = torch.bfloat16
+    a = dict(max_batch=2, max_pages=4, max_drafts=2)
+    a.update(sizes)
+    prefix = torch.zeros(64, 512, dtype=bf, device="cuda"), torch.zeros(64, 64, dtype=bf, device="cuda")
+    w = torch.zeros(16, 128, 512, dtype=bf, device="cuda")
+    with pytest.raises(ValueError, match="drafts"):
+        TyphoonMLADecoder(16, *prefix, w, w, 0.1, **a)
+    TyphoonMLADecoder(16, *prefix, w, w, 0.1, 2, 4, max_drafts=64).close()
+    TyphoonMLADecoder(16, *prefix, w, w, 0.1, 2, 0).close()
