@@ -331,7 +331,7 @@ int typhoon_mla_rope_init(typhoon_mla_rope_t* rope, int32_t d_rot, int32_t layou
     if (!rope || d_rot < 16 || d_rot > 64 || d_rot % 16) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (layout != TYPHOON_MLA_ROPE_INTERLEAVED && layout != TYPHOON_MLA_ROPE_HALF) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (scaling < TYPHOON_MLA_ROPE_SCALE_NONE || scaling > TYPHOON_MLA_ROPE_SCALE_YARN) return TYPHOON_MLA_ERR_INVALID_ARG;
-    if (!(base > 1.0) || !std::isfinite(base) || !std::isfinite(scale)) return TYPHOON_MLA_ERR_INVALID_ARG;
+    if (!(base > 1.0) || !std::isfinite(base) || !std::isfinite((float)scale)) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (scaling != TYPHOON_MLA_ROPE_SCALE_NONE && (!(factor >= 1.0) || !std::isfinite(factor))) return TYPHOON_MLA_ERR_INVALID_ARG;
     const double pi = 3.14159265358979323846, d = d_rot;
     double low = 0.0, high = 0.0;

@@ -26,3 +26,11 @@ def test_append_of_no_tokens_with_rotation(b):
     assert b._lib.typhoon_mla_cache_append(C.byref(bad), None, 512, None, 64, C.byref(r), None, None, 0, None, None) == 1
     r.d_rot = 20
     assert b._lib.typhoon_mla_cache_append(C.byref(c), None, 512, None, 64, C.byref(r), None, None, 0, None, None) == 1
+
+
+def test_rope_init_refuses_a_scale_that_is_infinite_in_32_bits(b):
+    """What rope_init accepts, the calls that take it accept."""
+    for scale in (1e39, -1e39):
+        with pytest.raises(b.TyphoonMLAError, match="invalid argument"):
+            b.typhoon_mla_rope_init(scale=scale)
+    assert b.typhoon_mla_rope_init(scale=3.4e38).scale > 3.3e38
