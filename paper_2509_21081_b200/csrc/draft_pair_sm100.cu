@@ -622,11 +622,11 @@ draft_pair_sm100_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_
                     tc_fence_after();
                     const uint32_t s_addr = tmem_base + lane_base + 256u + (uint32_t)((g & 1) * (E8 ? 128 : 64) + TPT * w);
                     uint32_t sr[TPT];
-                    tmem_ld_columns(s_addr, sr);
+                    tmem_ld32(s_addr, sr);
                     const uint64_t off2 = pack_f32x2(-base, -base), scale2 = pack_f32x2(p.scale_log2, p.scale_log2);
                     if (E8) {
                         uint32_t rr[TPT];
-                        tmem_ld_columns(s_addr + 64u, rr);
+                        tmem_ld32(s_addr + 64u, rr);
                         const uint64_t tau2 = pack_f32x2(tau * p.scale_log2, tau * p.scale_log2);
                         tmem_ld_wait();
 #pragma unroll

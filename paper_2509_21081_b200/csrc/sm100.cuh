@@ -520,16 +520,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
         : "r"(taddr)
         : "memory");
 }
-// 32 lanes x 16 columns, and either by the array's length
-__device__ __forceinline__ void tmem_ld_columns(uint32_t taddr, uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr)
-        : "memory");
-}
-__device__ __forceinline__ void tmem_ld_columns(uint32_t taddr, uint32_t (&r)[32]) { tmem_ld32(taddr, r); }
 // 16 lanes x 64 columns as accumulator fragments (measured layout): thread t of the warp gets, for every group g
 // of 8 columns, r[4g], r[4g+1] = lane (base + t/4), columns 8g + 2(t%4) + {0, 1} and r[4g+2], r[4g+3] = lane
 // (base + t/4 + 8), same columns.  All 32 threads hold data of the 16 lanes: the shape for M = 64 accumulators,
