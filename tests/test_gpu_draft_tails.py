@@ -70,3 +70,19 @@ def test_dominant_token_before_a_long_tail(bits, tokens, at, share, S, spread):
     assert status == 0
     assert torch.equal(got.view(copies, 2 * S, 16, 128), got[:2 * S].expand(copies, -1, -1, -1))
     check(got[:2 * S], want, lse[:2 * S], want_lse)
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+def test_dominant_token_before_a_quarter_of_a_million(bits):
+    """The longest tail here: 2^18 tokens in one piece, each worth 2^-18 of the dominant one."""
+    p = tailed(16, 1, 1 << 18, bits, 0.5, 0.0, 0, seed=47)
+    p.B, p.lens, p.table, p.slot = 1, p.lens[:1], p.table[:1], p.slot[:1]
+    p.q_nope, p.q_pe = p.q_nope[:1], p.q_pe[:1]
+    want, want_lse = p.reference()
+    copies = torch.cuda.get_device_properties(0).multi_processor_count // 2
+    dec = p.decoder(max_batch=copies)
+    p.B, p.lens, p.table = copies, p.lens * copies, p.table.repeat(copies, 1)
+    p.q_nope, p.q_pe = p.q_nope.repeat(copies, 1, 1), p.q_pe.repeat(copies, 1, 1)
+    got, lse, status = p.step(dec, mask=torch.ones(copies, 1, dtype=torch.int64))
+    assert status == 0 and torch.equal(got, got[:1].expand_as(got))
+    check(got[:1], want, lse[:1], want_lse)
