@@ -67,6 +67,9 @@ Settings snapshot() {
 
 inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// Arrays of 32-bit words (a misaligned one would fault in the kernel)
+template <typename... P>
+inline bool aligned4(const P*... p) { return (((reinterpret_cast<uintptr_t>(p) & 3u) == 0) && ...); }
 
 bool dims_supported(const typhoon_mla_dims_t& d) {
     return d.d_nope == 128 && d.d_rope == 64 && d.d_v == 128 && d.kv_lora_rank == 512 && d.num_heads >= 16 &&
@@ -1214,7 +1217,7 @@ static int decode_impl(const typhoon_mla_shared_t* sh, const void* q_nope, const
     const Settings cfg = snapshot();
     if (page_size != 64 && page_size != 128) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (mode < TYPHOON_MLA_MODE_AUTO || mode > TYPHOON_MLA_MODE_NAIVE) return TYPHOON_MLA_ERR_INVALID_ARG;
-    if (!aligned16(q_nope) || !aligned16(q_pe) || !aligned16(out)) return TYPHOON_MLA_ERR_INVALID_ARG;
+    if (!aligned16(q_nope) || !aligned16(q_pe) || !aligned16(out) || !aligned4(block_table, seq_lens, lse_out)) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (!(softmax_scale > 0.f) || softmax_scale > 3.0e38f) return TYPHOON_MLA_ERR_INVALID_ARG;   // positive, finite
     mode = resolve_mode(sh, B, max_pages, mode);
     const bool use_absorb = mode != TYPHOON_MLA_MODE_NAIVE;
@@ -1262,7 +1265,7 @@ int typhoon_mla_decode_partial(const typhoon_mla_shared_t* sh, const void* q_nop
 int typhoon_mla_combine_partials(const float* o_parts, const float* lse_parts, int32_t n_parts, int32_t B, int32_t H,
                                  void* out, float* lse_out, void* stream) {
     if (!o_parts || !lse_parts || !out || n_parts < 1 || B < 1 || H < 1) return TYPHOON_MLA_ERR_INVALID_ARG;
-    if (!aligned16(o_parts) || !aligned16(out)) return TYPHOON_MLA_ERR_INVALID_ARG;
+    if (!aligned16(o_parts) || !aligned16(out) || !aligned4(lse_parts, lse_out)) return TYPHOON_MLA_ERR_INVALID_ARG;
     tmla::tl_pdl = g_pdl.load();
     const cudaError_t e = launch_combine(o_parts, lse_parts, n_parts, nullptr, nullptr, B, H, out, lse_out,
                                          reinterpret_cast<cudaStream_t>(stream));
@@ -1295,6 +1298,7 @@ int typhoon_mla_decode_draft(const typhoon_mla_shared_t* sh, const void* q_nope,
     if (!q_nope || !q_pe || !out || !block_table || !seq_lens) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (!on_handle_device(sh)) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (!aligned16(q_nope) || !aligned16(q_pe) || !aligned16(out) || (reinterpret_cast<uintptr_t>(tree_mask) & 7u)) return TYPHOON_MLA_ERR_INVALID_ARG;
+    if (!aligned4(block_table, seq_lens, draft_lens, lse_out)) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (!(softmax_scale > 0.f) || softmax_scale > 3.0e38f) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return TYPHOON_MLA_ERR_INVALID_ARG;
     const Settings cfg = snapshot();
@@ -1438,7 +1442,7 @@ int typhoon_mla_decode_tree(const typhoon_mla_prefix_level_t* levels, int32_t n_
     g_last_launches = 0;
     if (!q_nope || !q_pe || !out || B < 1 || max_pages < 0) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (page_size != 64 && page_size != 128) return TYPHOON_MLA_ERR_INVALID_ARG;
-    if (!aligned16(q_nope) || !aligned16(q_pe) || !aligned16(out)) return TYPHOON_MLA_ERR_INVALID_ARG;
+    if (!aligned16(q_nope) || !aligned16(q_pe) || !aligned16(out) || !aligned4(block_table, seq_lens, lse_out)) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (!(softmax_scale > 0.f) || softmax_scale > 3.0e38f) return TYPHOON_MLA_ERR_INVALID_ARG;
     const Settings cfg = snapshot();
     if (!cfg.tc()) return TYPHOON_MLA_ERR_UNSUPPORTED_DIMS;
