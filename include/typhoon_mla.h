@@ -470,7 +470,7 @@ int typhoon_mla_cache_read(const typhoon_mla_cache_t* cache /* host */, const in
  * 2^-27 of that below; an element of the absorbed query to 2^-8 of itself down to 2^-10 of the row's largest, and to 2^-18 of that
  * below (values below 2^-90 of magnitude count as zeros in the output).
  * B * S <= TYPHOON_MLA_MAX_DRAFT_ROWS; tcgen05 kernel path only (UNSUPPORTED_DIMS otherwise); streams, capture and errors as
- * typhoon_mla_decode.
+ * typhoon_mla_decode (over an 8-bit cache the handle's side stream is used in ABSORB mode as well).
  */
 #define TYPHOON_MLA_MAX_DRAFT_ROWS (1 << 20)
 int typhoon_mla_decode_draft(const typhoon_mla_shared_t* shared, const void* q_nope, const void* q_pe, int32_t B, int32_t S,

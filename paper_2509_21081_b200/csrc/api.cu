@@ -1088,8 +1088,8 @@ static int decode_core(const Settings& cfg, const typhoon_mla_shared* sh, const 
                 q_terms = pl.n_shared_chunks > 0 ? ws + pl.off_olat : q_abs;
                 q_tau = o_abs;   // (the warp-MMA path's)
             }
-            e = launch_q_absorb_sm100(q_nope, &sh->tm_wuk_t, q_terms == q_abs ? nullptr : q_abs, B, H, sh->num_sms, walk_ctas, sh->status, order ? seq_lens : nullptr, order,
-                                      block_table, max_pages, page_size, desc, s, n_requests, q_terms, q_tau);
+            e = launch_q_absorb_sm100(q_nope, &sh->tm_wuk_t, q_terms == q_abs ? nullptr : q_abs, B, H, sh->num_sms, walk_ctas, sh->status,
+                                      order ? seq_lens : nullptr, order, block_table, max_pages, page_size, desc, s, n_requests, q_terms, q_tau);
         } else {
             GemmTN g1{q_nope, (int64_t)H * 128, 128, sh->w_uk_t, 128, 512 * 128, q_abs, (int64_t)H * 512, 512,
                       B, 512, 128, H, false};
@@ -1297,8 +1297,8 @@ int typhoon_mla_decode_draft(const typhoon_mla_shared_t* sh, const void* q_nope,
     if (!draft_sizes_valid(sh, B, S, max_pages, mode) || !cache_valid(cache)) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (!q_nope || !q_pe || !out || !block_table || !seq_lens) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (!on_handle_device(sh)) return TYPHOON_MLA_ERR_INVALID_ARG;
-    if (!aligned16(q_nope) || !aligned16(q_pe) || !aligned16(out) || (reinterpret_cast<uintptr_t>(tree_mask) & 7u)) return TYPHOON_MLA_ERR_INVALID_ARG;
-    if (!aligned4(block_table, seq_lens, draft_lens, lse_out)) return TYPHOON_MLA_ERR_INVALID_ARG;
+    if (!aligned16(q_nope) || !aligned16(q_pe) || !aligned16(out)) return TYPHOON_MLA_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(tree_mask) & 7u) || !aligned4(block_table, seq_lens, draft_lens, lse_out)) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (!(softmax_scale > 0.f) || softmax_scale > 3.0e38f) return TYPHOON_MLA_ERR_INVALID_ARG;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return TYPHOON_MLA_ERR_INVALID_ARG;
     const Settings cfg = snapshot();

@@ -39,12 +39,13 @@
 // the even CTA issues both products (in the odd one it requests W_UV into L2); warp 3 turns the tokens' exponent bytes into floats;
 // warps 4-11: softmax and epilogue, a thread per row and 32 tokens of a tile.
 //
-// What bounds it (B200; 64 requests of 1024 rows over 2112 tokens each, 16 / 8 bits: 236 / 281 us, 1.28 / 1.07 PFLOP/s; 74 requests of
-// 128 rows over 4096 tokens that nobody shares 74 / 82 us; 296 of 128 rows over 512 tokens 61 / 66; one tile per pair 12.8 / 14.0):
+// What bounds it (B200; 64 requests of 1024 rows over 2112 tokens each, 16 / 8 bits: 236 / 327 us, 1.27 / 0.92 PFLOP/s; 74 requests of
+// 128 rows over 4096 tokens that nobody shares 75 / 96 us; 296 of 128 rows over 512 tokens 61 / 71; one tile per pair 12.8 / 14.5):
 //   - 16 bits: a tile takes 2480 clocks, 2176 of them products; the rest is the reload of V, for which there is one stage (K, V, Q and P
 //     fill shared memory; 136 KB come from L2 per CTA and tile).
-//   - 8 bits: 3600 clocks for 2600 of products (two terms of P: 3100 for 2100): the softmax warps' own chain (two per scheduler, in step by the vote).  Sixteen of them
-//     with half the tokens each take as long; requesting the next logits earlier needs more registers than there are.
+//   - 8 bits: 3600 clocks for 2600 of products: the softmax warps' own chain (two per scheduler, in step by the vote).  Sixteen of them
+//     with half the tokens each take as long; requesting the next logits earlier needs more registers than there are.  The third term
+//     of P costs 12 % of the first shape above, half of it as products, half in the softmax warps (two terms of 3 bits would do without).
 //   - an item costs 7000 clocks beside its tiles: result 3000, last product 1100, drafts' values read through 1000, first logits 1000.
 //     Hence pairs that walk through items with loads one item ahead (one item per pair and launch: 10 us each).
 #include <algorithm>
@@ -982,7 +983,8 @@ cudaError_t launch_draft_sm100(const DraftAttn& a, void* o_lat_direct, float* ls
     tm_ckv_sh = tm_ckv;
     tm_kpe_sh = tm_kpe;
     if (a.n_sh_chunks > 0) {
-        const typhoon_mla_cache_t prefix{const_cast<void*>(a.ckv_shared), const_cast<void*>(a.kpe_shared), nullptr, 512, 64, 64, (int32_t)(a.Ls_pad / 64)};
+        const typhoon_mla_cache_t prefix{const_cast<void*>(a.ckv_shared), const_cast<void*>(a.kpe_shared), nullptr, 512, 64, 64,
+                                         (int32_t)(a.Ls_pad / 64)};
         e = make_kv_tmaps(prefix, &tm_ckv_sh, &tm_kpe_sh);
         if (e != cudaSuccess) return e;
     }
@@ -1007,7 +1009,8 @@ cudaError_t launch_draft_sm100(const DraftAttn& a, void* o_lat_direct, float* ls
     p.l2_total = a.w_uv ? (uint32_t)std::min<int64_t>((int64_t)a.H * 128 * 512 * 2, (int64_t)pairs * 32 * 4096) : 0u;
     p.l2_bytes = (p.l2_total / (pairs * 32u) / 16u + 1u) * 16u;
     auto* kernel = e8 ? draft_pair_sm100_kernel<true> : draft_pair_sm100_kernel<false>;
-    return launch_pdl(kernel, dim3((unsigned)(2 * pairs)), dim3(e8 ? Shape<true>::THREADS : Shape<false>::THREADS), kDraftSmem, s, tm_qa, tm_qp, tm_ckv, tm_kpe, tm_ckv_sh, tm_kpe_sh, p);
+    const dim3 block(e8 ? Shape<true>::THREADS : Shape<false>::THREADS);
+    return launch_pdl(kernel, dim3((unsigned)(2 * pairs)), block, kDraftSmem, s, tm_qa, tm_qp, tm_ckv, tm_kpe, tm_ckv_sh, tm_kpe_sh, p);
 }
 
 }  // namespace tmla
